@@ -19,6 +19,13 @@
  *   wushkv_decode_attention  Alg. 2 steps 3 (queries) and 5, Eq. (2)
  *   wushkv_dequant           the reconstruction of Eq. (7) for stored tokens
  *   wushkv_wush_transform    the transform T of Eq. (1) (calibration, Alg. 1)
+ * and, beyond the paper, for serving from one pool of pages:
+ *   wushkv_page_bounds, wushkv_select_pages, wushkv_sparse_attention
+ *                            attention over the pages that a bound on their
+ *                            logits selects for each decode query
+ *   wushkv_assign_pages, wushkv_compact_pages
+ *                            sequences freed, forked and given pages; the
+ *                            pages in use moved to the front of the pool
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless marked (host), and must be
@@ -132,6 +139,10 @@ enum {
  *   (the operand order of the 16x16x32 fp16 product: a few shifts and one
  *   mask per operand register move each code near the top of an fp16
  *   fraction).
+ *
+ *   What a page holds for positions that are not quantised yet may be any bit
+ *   pattern (a page taken again keeps its old bytes); it is never read into a
+ *   result.
  *
  * win_k: bf16 [batch][n_kv_heads][win_slots][head_dim]   (token-major)
  * win_v: bf16 [batch][n_kv_heads][head_dim][win_slots]   (channel-major)
@@ -395,6 +406,175 @@ size_t wushkv_chunk_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads,
 int wushkv_dequant(const wushkv_cache *c, int32_t b, int32_t start,
                    int32_t count, float *k_out, float *v_out,
                    wushkv_stream_t stream);
+
+/*
+ * Page bounds: for every complete page (all 64 positions quantised, so that it
+ * does not change any more) and kv head a box round its stored keys in 8 bits,
+ * kept per PHYSICAL page, so that sequences sharing a page share its box.
+ *   codes   int8 [n_pages][n_kv_heads][2][head_dim]: the box's centres, then
+ *           its radii (0..127), per channel.
+ *   scales  fp32 [n_kv_heads][n_pages]: a channel spans
+ *           scale (centre - radius) .. scale (centre + radius).
+ */
+typedef struct wushkv_bounds {
+    int8_t *codes;
+    float *scales;
+} wushkv_bounds;
+
+/*
+ * wushkv_page_bounds -- the boxes of the pages completed since the last call.
+ *
+ *   since    int32 [batch] device, or NULL for 0 everywhere: quant_end[b] as it
+ *            was when sequence b's boxes were last up to date.  The call builds
+ *            the boxes of the logical pages complete now that were not then.
+ *   max_new  (host) >= the number of such pages of every sequence, sizes the
+ *            grid (more are left out); 0 is a no-op.
+ *
+ * With x_tj = scale_t code_tj + zero_t the page's stored keys (fp32 fma), over
+ * the page's 64 tokens t, each step one correctly rounded fp32 operation:
+ *   lo_j = min_t x_tj, hi_j = max_t x_tj, a = max_j max(|lo_j|, |hi_j|);
+ *   s = a / 126;  centre_j = rne(((lo_j + hi_j) 0.5) / s);
+ *   radius_j = min(127, ceil(max(hi_j - centre_j s, centre_j s - lo_j) / s)).
+ * A page of zeros gets s = 0 and zero codes.  A page with a key scale or zero
+ * that is not finite gets s = +inf and zero codes: it is selected first.
+ * A logical page whose physical index lies outside the pool is skipped.
+ */
+int wushkv_page_bounds(const wushkv_cache *c, const wushkv_bounds *bounds, const int32_t *since,
+                       int32_t max_new, wushkv_stream_t stream);
+
+/*
+ * wushkv_select_pages -- for each (sequence, kv head) the complete pages with
+ * the largest bound on a logit of the decode query, and the page being filled.
+ *
+ *   q, n_q_heads, t_k_inv  as wushkv_decode_attention takes them.
+ *   max_seq_len  (host) >= every seq_len[b] (pages beyond it are left out);
+ *            sizes the grid and the workspace.
+ *   top_k    (host) >= 0: complete pages selected per (sequence, kv head).
+ *   sel      int32 [batch][n_kv_heads][top_k + 1]: logical pages, ascending;
+ *            -1 from n_sel on.
+ *   n_sel    int32 [batch][n_kv_heads]: min(top_k, complete pages) + 1 if the
+ *            sequence's last page is partly quantised.
+ *   scores   nullable fp32 [batch][n_kv_heads][max_pages_per_seq]: the scores
+ *            of the complete pages (entries behind them are left as they are).
+ *   workspace  wushkv_select_workspace_bytes() bytes, not initialised.
+ *
+ * With q~ = q t_k_inv (fp64), F = 14 - ex, max_j |q~_j| in [2^(ex-1), 2^ex),
+ * F clamped to [-100, 100], and N_j = rne(q~_j 2^F) clamped to +-16384:
+ *   score(page) = max over the group's query heads of
+ *                 ((fp32) sum_j (N_j centre_j + |N_j| radius_j) scale) 2^-F,
+ * the sum exact, every other step one rounded fp32 operation.  For a positive
+ * softmax scale it bounds q~ . k over the page's stored keys k from above, up
+ * to the rounding of q~ to 15 bits and of the steps above.  A page
+ * of infinite scale scores +inf, one outside the pool -inf; a query head whose
+ * q~ is not finite counts as zero.  Of equal scores the lowest page is taken.
+ * Complete pages whose boxes were never built score by what is stored there.
+ */
+int wushkv_select_pages(const wushkv_cache *c, const wushkv_bounds *bounds, const uint16_t *q,
+                        int32_t n_q_heads, int32_t max_seq_len, const float *t_k_inv,
+                        int32_t top_k, int32_t *sel, int32_t *n_sel, float *scores,
+                        void *workspace, size_t workspace_bytes, wushkv_stream_t stream);
+
+/* Workspace of wushkv_select_pages, or 0 for invalid arguments. */
+size_t wushkv_select_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads,
+                                     int32_t max_seq_len, int32_t top_k);
+
+/*
+ * wushkv_sparse_attention -- wushkv_decode_attention over listed pages: each
+ * query attends to the sink, to the recent window and, of the quantised
+ * positions, to those in the listed pages of its (sequence, kv head).
+ *
+ *   sel      int32 [batch][n_kv_heads][max_sel]: logical pages, in any order.
+ *            Of an entry's page the quantised positions count.  An entry
+ *            outside [0, max_pages_per_seq), or whose page is outside the pool,
+ *            contributes nothing; a page listed twice counts twice.
+ *   n_sel    int32 [batch][n_kv_heads]: entries used, clamped to [0, max_sel].
+ *   max_sel  (host) >= 0, the row length of sel; sizes the grid.
+ *   The other arguments are wushkv_decode_attention's; the workspace needs
+ *   wushkv_sparse_workspace_bytes().
+ * A sequence with seq_len 0 gets zeros.  Returns WUSHKV_EUNSUPPORTED where
+ * max_sel pages would need a run longer than 64 pages per wave (about 262 000).
+ */
+int wushkv_sparse_attention(const wushkv_cache *c, const uint16_t *q, int32_t n_q_heads,
+                            const int32_t *sel, const int32_t *n_sel, int32_t max_sel,
+                            const float *t_k_inv, float sm_scale, float *out, void *workspace,
+                            size_t workspace_bytes, wushkv_stream_t stream);
+
+/* Workspace of wushkv_sparse_attention, or 0 for invalid arguments. */
+size_t wushkv_sparse_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads, int32_t max_sel);
+
+/*
+ * A pool's bookkeeping, for caches whose sequences share one pool of pages.
+ *   refs   int32 [n_pages]: page-table rows that hold the page; 0: free.  A page
+ *          the caller adds a reference to is not handed out or freed.
+ *   held   int32 [batch]: pages sequence b holds: its page-table row is valid in
+ *          [0, held[b]) and not read beyond.
+ *   low    int32 [1]: no page below low[0] is free (0 is always right; kept so
+ *          that the search for free pages starts there).
+ */
+typedef struct wushkv_pool {
+    int32_t *refs;
+    int32_t *held;
+    int32_t *low;
+} wushkv_pool;
+
+/*
+ * wushkv_assign_pages -- frees, forks and extends sequences, in this order,
+ * for the whole batch at once.
+ *
+ *   source  int32 [batch] device, or NULL (every sequence keeps its state).
+ *           source[b] = b   sequence b is kept;
+ *           source[b] = -1  freed: its references are dropped, its row becomes
+ *                           -1, seq_len, quant_end and held 0;
+ *           source[b] = s   (another sequence that is itself kept): freed, then
+ *                           a copy of s: it shares s's complete pages, gets a
+ *                           page of its own for s's partly quantised page, and
+ *                           copies that page, the windows (every slot), seq_len
+ *                           and quant_end.  Several may copy the same s.
+ *           Anything else is refused: b is kept and status[b] is negative.
+ *   reach   int32 [batch] device, or NULL: sequence b gets pages so that it
+ *           holds those of all positions below reach[b] (at most
+ *           max_pages_per_seq; it never loses pages).  A freed sequence may
+ *           reach too.
+ *   status  int32 [batch]: the number of pages missing because the pool ran
+ *           out (their entries are -1 and held ends before them), or, where
+ *           source[b] was refused, -1 minus that number.  A fork whose own page
+ *           is missing lacks the positions in it.
+ *
+ * Pages are handed out in the order of the sequences and, for each, of its
+ * logical pages, the lowest free one first: the result depends on nothing else.
+ * The boxes of complete pages are shared with the pages.  Complete pages are
+ * never written to, so shared pages need no later copy (a sequence must not be
+ * set back, by its counters, into a page that another one holds).  The pages, windows,
+ * counters, page table and pool of the whole batch must not be in use on
+ * another stream.  A batch above 16384 is WUSHKV_EUNSUPPORTED.
+ */
+int wushkv_assign_pages(const wushkv_cache *c, const wushkv_pool *pool, const int32_t *source,
+                        const int32_t *reach, int32_t *status, wushkv_stream_t stream);
+
+/*
+ * wushkv_compact_pages -- moves pages so that the n pages in use (refs > 0)
+ * are the physical pages 0 .. n - 1: the i-th free page below n takes the i-th
+ * used page from n on (its data for all kv heads, and its boxes).
+ *
+ *   bounds     nullable: the boxes that move with the pages.
+ *   table_out  int32 [batch][max_pages_per_seq]: the new page table: entries in
+ *              [0, held[b]) that lie in the pool renumbered, the others -1.
+ *   refs_out   int32 [n_pages]: the new references, 0 from n on.
+ *              Either may be the cache's, or the pool's, own array (in place).
+ *              Into other arrays the call leaves the old table and references
+ *              valid: no page they name is overwritten, so that reads through
+ *              them may still run until the caller swaps them in.
+ *   live_out   nullable int32 [1]: n.
+ *   workspace  wushkv_compact_workspace_bytes() bytes, not initialised.
+ * pool->low stays right in both cases.
+ */
+int wushkv_compact_pages(const wushkv_cache *c, const wushkv_pool *pool,
+                         const wushkv_bounds *bounds, int32_t *table_out, int32_t *refs_out,
+                         int32_t *live_out, void *workspace, size_t workspace_bytes,
+                         wushkv_stream_t stream);
+
+/* Workspace of wushkv_compact_pages, or 0 for invalid arguments. */
+size_t wushkv_compact_workspace_bytes(const wushkv_cache *c);
 
 /* Name of a status code. */
 const char *wushkv_status_string(int status);

@@ -17,7 +17,7 @@ import math
 import operator
 
 from . import _lib
-from ._lib import (CacheDesc, WushKVError, PAGE_TOKENS, check, header_functions,
+from ._lib import (BoundsDesc, CacheDesc, PoolDesc, WushKVError, PAGE_TOKENS, check, header_functions,
                    status_string)
 
 __all__ = [
@@ -26,6 +26,9 @@ __all__ = [
     "wushkv_decode_workspace_bytes", "wushkv_dequant", "wushkv_page_bytes",
     "wushkv_status_string", "wushkv_abi_version", "wushkv_timing_enable",
     "wushkv_timing_read", "wushkv_timing_launches", "wushkv_quest_alpha", "wushkv_wush_transform", "wushkv_read_probe",
+    "WushKVBounds", "WushKVPool", "wushkv_page_bounds", "wushkv_select_pages",
+    "wushkv_select_workspace_bytes", "wushkv_sparse_attention", "wushkv_sparse_workspace_bytes",
+    "wushkv_assign_pages", "wushkv_compact_pages", "wushkv_compact_workspace_bytes",
     "PAGE_TOKENS",
     "header_functions",
 ]
@@ -106,14 +109,17 @@ class WushKVCache:
     only read where live).
     ``page_order`` "linear" maps logical page i of sequence b to physical
     page b * max_pages + i; "random" draws a seeded permutation of a pool
-    ``pool_factor`` times the needed size.  ``codec`` is "pclip" (Eq. (7),
+    ``pool_factor`` times the needed size, "none" leaves the table empty (-1)
+    for wushkv_assign_pages to fill from a pool of ``n_pages`` pages (by
+    default as many as the other orders take).  ``codec`` is "pclip" (Eq. (7),
     clip quantiles kappa_k / kappa_v) or "quest" (Eq. (5), clip multiplier
     ``quest_alpha``, by default the library's wushkv_quest_alpha(bits)).
     """
 
     def __init__(self, batch, n_kv_heads, head_dim, bits, s_sink, s_keep, s_flush,
                  kappa_k, kappa_v, max_seq_len, win_slots=None, page_order="linear",
-                 pool_factor=1.0, seed=0, device="cuda", codec="pclip", quest_alpha=None):
+                 pool_factor=1.0, seed=0, device="cuda", codec="pclip", quest_alpha=None,
+                 n_pages=None):
         torch = _torch()
         self.batch, self.n_kv_heads, self.head_dim, self.bits = batch, n_kv_heads, head_dim, bits
         self.s_sink, self.s_keep, self.s_flush = s_sink, s_keep, s_flush
@@ -133,6 +139,10 @@ class WushKVCache:
         self.max_pages = max(1, math.ceil(max(0, max_seq_len - s_sink) / PAGE_TOKENS))
         need_pages = batch * self.max_pages
         self.n_pages = max(need_pages, int(math.ceil(need_pages * pool_factor)))
+        if n_pages is not None:
+            if page_order != "none":
+                raise ValueError("n_pages goes with page_order=\"none\"")
+            self.n_pages = int(n_pages)
         self.page_bytes = wushkv_page_bytes(head_dim, bits)
         if self.page_bytes == 0:
             raise WushKVError(_lib.EUNSUPPORTED, "WushKVCache")
@@ -145,6 +155,8 @@ class WushKVCache:
         elif page_order == "random":
             g = torch.Generator().manual_seed(seed)
             table = torch.randperm(self.n_pages, generator=g)[:need_pages].to(torch.int32)
+        elif page_order == "none":
+            table = torch.full((need_pages,), -1, dtype=torch.int32)
         else:
             raise ValueError(page_order)
         self.page_table = table.reshape(batch, self.max_pages).contiguous().to(dev)
@@ -178,6 +190,42 @@ class WushKVCache:
             setattr(new, name, getattr(self, name).clone())
         new._desc = new._make_desc()
         return new
+
+
+class WushKVBounds:
+    """The boxes of a cache's complete pages (wushkv_page_bounds): ``codes``
+    int8 [n_pages][n_kv][2][d], centres then radii, and ``scales`` fp32
+    [n_kv][n_pages], zero-initialised on the cache's device."""
+
+    def __init__(self, cache: WushKVCache):
+        torch = _torch()
+        self.codes = torch.zeros(cache.n_pages, cache.n_kv_heads, 2, cache.head_dim, dtype=torch.int8,
+                                 device=cache.device)
+        self.scales = torch.zeros(cache.n_kv_heads, cache.n_pages, dtype=torch.float32, device=cache.device)
+        self._desc = BoundsDesc(self.codes.data_ptr(), self.scales.data_ptr())
+
+    @property
+    def desc(self) -> BoundsDesc:
+        return self._desc
+
+
+class WushKVPool:
+    """The bookkeeping of a cache's pages (wushkv_assign_pages): ``refs`` int32
+    [n_pages], ``held`` int32 [batch] and ``low`` int32 [1].  Starts from the
+    cache's page table: every entry of it is one reference."""
+
+    def __init__(self, cache: WushKVCache):
+        torch = _torch()
+        there = (cache.page_table >= 0) & (cache.page_table < cache.n_pages)
+        self.held = there.sum(1, dtype=torch.int32)
+        pages = cache.page_table[there].long()
+        self.refs = torch.bincount(pages, minlength=cache.n_pages).to(torch.int32)
+        self.low = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        self._desc = PoolDesc(self.refs.data_ptr(), self.held.data_ptr(), self.low.data_ptr())
+
+    @property
+    def desc(self) -> PoolDesc:
+        return self._desc
 
 
 def _check_2byte(t, name):
@@ -367,6 +415,169 @@ def wushkv_dequant(cache: WushKVCache, b: int, start: int, count: int, k_out=Non
                                    _ptr(k_out), _ptr(v_out), _stream_handle(stream))
     check(st, "wushkv_dequant")
     return k_out, v_out
+
+
+def _check(cache, t, name, dtype, shape, optional=False):
+    """A contiguous tensor of this type and shape on the cache's device."""
+    if t is None and optional:
+        return
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, list(shape)))
+    if t.device != cache.pages.device:
+        raise ValueError("%s is not on the cache's device" % name)
+
+
+def _launch_stream(cache, stream):
+    """The stream handle of a call on the cache's device, which has to be the
+    current one."""
+    if cache.pages.device.index != _torch().cuda.current_device():
+        raise ValueError("the cache's device is not the current one")
+    return _stream_handle(stream)
+
+
+def _on_stream(t, stream):
+    """A buffer made here for a call on another stream than the current one
+    stays allocated until that stream has done with it."""
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def wushkv_page_bounds(cache: WushKVCache, bounds: WushKVBounds, since=None, max_new=None, stream=None) -> None:
+    """The boxes of the pages completed since quant_end was ``since`` (int32
+    [batch] on the device; None: of all complete pages), at most ``max_new``
+    (by default max_pages) a sequence."""
+    torch = _torch()
+    _check(cache, since, "since", torch.int32, (cache.batch,), True)
+    st = _lib.lib().wushkv_page_bounds(
+        ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(since),
+        cache.max_pages if max_new is None else operator.index(max_new), _launch_stream(cache, stream))
+    check(st, "wushkv_page_bounds")
+
+
+def wushkv_select_workspace_bytes(cache: WushKVCache, n_q_heads: int, max_seq_len: int, top_k: int) -> int:
+    return _lib.lib().wushkv_select_workspace_bytes(ctypes.byref(cache.desc), n_q_heads, max_seq_len, top_k)
+
+
+def wushkv_select_pages(cache: WushKVCache, bounds: WushKVBounds, q, t_k_inv, top_k, max_seq_len=None, sel=None,
+                        n_sel=None, scores=None, workspace=None, stream=None):
+    """For each (sequence, kv head) the ``top_k`` complete pages with the
+    largest bound on a logit of the query, and the page being filled.  q: bf16
+    [batch][n_q][d]; t_k_inv: fp32 [n_kv][d][d].  Returns (sel int32
+    [batch][n_kv][top_k + 1], ascending, -1 behind; n_sel int32
+    [batch][n_kv]); ``scores``, if given, fp32 [batch][n_kv][max_pages],
+    receives every complete page's score."""
+    torch = _torch()
+    b, hk, d, top_k = cache.batch, cache.n_kv_heads, cache.head_dim, operator.index(top_k)
+    n_q = q.shape[1] if q.dim() == 3 else 0
+    _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
+    _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    _check(cache, scores, "scores", torch.float32, (b, hk, cache.max_pages), True)
+    if max_seq_len is None:
+        max_seq_len = cache.max_seq_len
+    need = wushkv_select_workspace_bytes(cache, n_q, operator.index(max_seq_len), top_k)
+    handle = _launch_stream(cache, stream)
+    if need:  # (otherwise the call says what is wrong)
+        if sel is None:
+            sel = _on_stream(torch.empty(b, hk, top_k + 1, dtype=torch.int32, device=q.device), stream)
+        if n_sel is None:
+            n_sel = _on_stream(torch.empty(b, hk, dtype=torch.int32, device=q.device), stream)
+        if workspace is None:
+            workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+        _check(cache, sel, "sel", torch.int32, (b, hk, top_k + 1))
+        _check(cache, n_sel, "n_sel", torch.int32, (b, hk))
+    st = _lib.lib().wushkv_select_pages(
+        ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(q), n_q, operator.index(max_seq_len),
+        _ptr(t_k_inv), top_k, _ptr(sel), _ptr(n_sel), _ptr(scores), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), handle)
+    check(st, "wushkv_select_pages")
+    return sel, n_sel
+
+
+def wushkv_sparse_workspace_bytes(cache: WushKVCache, n_q_heads: int, max_sel: int) -> int:
+    return _lib.lib().wushkv_sparse_workspace_bytes(ctypes.byref(cache.desc), n_q_heads, max_sel)
+
+
+def wushkv_sparse_attention(cache: WushKVCache, q, t_k_inv, sel, n_sel, sm_scale=None, out=None, workspace=None,
+                            stream=None):
+    """wushkv_decode_attention over the sink, the recent window and the listed
+    pages: sel int32 [batch][n_kv][max_sel] logical pages, of which the first
+    n_sel (int32 [batch][n_kv]) count.  Returns fp32 [batch][n_q][d]."""
+    torch = _torch()
+    b, hk, d = cache.batch, cache.n_kv_heads, cache.head_dim
+    n_q = q.shape[1] if q.dim() == 3 else 0
+    max_sel = sel.shape[2] if sel.dim() == 3 else 0
+    _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
+    _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    _check(cache, sel, "sel", torch.int32, (b, hk, max_sel))
+    _check(cache, n_sel, "n_sel", torch.int32, (b, hk))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    handle = _launch_stream(cache, stream)
+    if out is None:
+        out = _on_stream(torch.empty(b, n_q, d, dtype=torch.float32, device=q.device), stream)
+    _check(cache, out, "out", torch.float32, (b, n_q, d))
+    if workspace is None:
+        # (sizes without a plan: the call says what is wrong)
+        need = max(16, wushkv_sparse_workspace_bytes(cache, n_q, max_sel))
+        workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+    st = _lib.lib().wushkv_sparse_attention(
+        ctypes.byref(cache.desc), _ptr(q), n_q, _ptr(sel), _ptr(n_sel), max_sel, _ptr(t_k_inv), float(sm_scale),
+        _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
+    check(st, "wushkv_sparse_attention")
+    return out
+
+
+def wushkv_assign_pages(cache: WushKVCache, pool: WushKVPool, source=None, reach=None, status=None, stream=None):
+    """Frees, forks and extends sequences: source[b] = b keeps sequence b, -1
+    frees it, s makes it a copy of the kept sequence s (None keeps all);
+    reach[b]: positions it is to hold pages for (None: no new ones).  Both
+    int32 [batch] on the device.  Returns status int32 [batch]: pages missing,
+    or -1 minus that where source[b] was refused."""
+    torch = _torch()
+    shape = (cache.batch,)
+    _check(cache, source, "source", torch.int32, shape, True)
+    _check(cache, reach, "reach", torch.int32, shape, True)
+    handle = _launch_stream(cache, stream)
+    if status is None:
+        status = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
+    _check(cache, status, "status", torch.int32, shape)
+    st = _lib.lib().wushkv_assign_pages(ctypes.byref(cache.desc), ctypes.byref(pool.desc), _ptr(source), _ptr(reach),
+                                        _ptr(status), handle)
+    check(st, "wushkv_assign_pages")
+    return status
+
+
+def wushkv_compact_workspace_bytes(cache: WushKVCache) -> int:
+    return _lib.lib().wushkv_compact_workspace_bytes(ctypes.byref(cache.desc))
+
+
+def wushkv_compact_pages(cache: WushKVCache, pool: WushKVPool, bounds=None, table_out=None, refs_out=None,
+                         live_out=None, workspace=None, stream=None):
+    """Moves the n pages in use to the physical pages 0 .. n - 1 (with their
+    boxes, if bounds is given).  The page table and references change in place
+    or, where table_out and refs_out are given, into those.  Returns (page
+    table, references, n as int32 [1]), on the device."""
+    torch = _torch()
+    handle = _launch_stream(cache, stream)
+    if table_out is None:
+        table_out = cache.page_table
+    if refs_out is None:
+        refs_out = pool.refs
+    if live_out is None:
+        live_out = _on_stream(torch.empty(1, dtype=torch.int32, device=cache.device), stream)
+    _check(cache, table_out, "table_out", torch.int32, (cache.batch, cache.max_pages))
+    _check(cache, refs_out, "refs_out", torch.int32, (cache.n_pages,))
+    _check(cache, live_out, "live_out", torch.int32, (1,))
+    if workspace is None:
+        need = max(16, wushkv_compact_workspace_bytes(cache))
+        workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=cache.device), stream)
+    st = _lib.lib().wushkv_compact_pages(
+        ctypes.byref(cache.desc), ctypes.byref(pool.desc), None if bounds is None else ctypes.byref(bounds.desc),
+        _ptr(table_out), _ptr(refs_out), _ptr(live_out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), handle)
+    check(st, "wushkv_compact_pages")
+    return table_out, refs_out, live_out
 
 
 def wushkv_wush_transform(m, h, gamma: float = 1e-2, t_out=None, t_inv_out=None,

@@ -47,6 +47,16 @@ class CacheDesc(ctypes.Structure):
     ]
 
 
+class BoundsDesc(ctypes.Structure):
+    """Mirror of struct wushkv_bounds."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class PoolDesc(ctypes.Structure):
+    """Mirror of struct wushkv_pool."""
+    _fields_ = [("refs", ctypes.c_void_p), ("held", ctypes.c_void_p), ("low", ctypes.c_void_p)]
+
+
 class WushKVError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -98,6 +108,23 @@ def _declare(L):
     L.wushkv_abi_version.restype = ctypes.c_int
     L.wushkv_wush_transform.argtypes = [P, P, I32, I32, F32, P, P, P, P]
     L.wushkv_wush_transform.restype = ctypes.c_int
+    B, O = ctypes.POINTER(BoundsDesc), ctypes.POINTER(PoolDesc)
+    L.wushkv_page_bounds.argtypes = [D, B, P, I32, P]
+    L.wushkv_page_bounds.restype = ctypes.c_int
+    L.wushkv_select_pages.argtypes = [D, B, P, I32, I32, P, I32, P, P, P, P, SZ, P]
+    L.wushkv_select_pages.restype = ctypes.c_int
+    L.wushkv_select_workspace_bytes.argtypes = [D, I32, I32, I32]
+    L.wushkv_select_workspace_bytes.restype = SZ
+    L.wushkv_sparse_attention.argtypes = [D, P, I32, P, P, I32, P, F32, P, P, SZ, P]
+    L.wushkv_sparse_attention.restype = ctypes.c_int
+    L.wushkv_sparse_workspace_bytes.argtypes = [D, I32, I32]
+    L.wushkv_sparse_workspace_bytes.restype = SZ
+    L.wushkv_assign_pages.argtypes = [D, O, P, P, P, P]
+    L.wushkv_assign_pages.restype = ctypes.c_int
+    L.wushkv_compact_pages.argtypes = [D, O, B, P, P, P, P, SZ, P]
+    L.wushkv_compact_pages.restype = ctypes.c_int
+    L.wushkv_compact_workspace_bytes.argtypes = [D]
+    L.wushkv_compact_workspace_bytes.restype = SZ
     L.wushkv_read_probe.argtypes = [P, SZ, I32, P, P]
     L.wushkv_read_probe.restype = ctypes.c_int
     L.wushkv_quest_alpha.argtypes = [I32]

@@ -19,7 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libwushkv.so")
-SOURCES = ["api.hip", "append.hip", "decode.hip", "dequant.hip", "wush.hip", "probe.hip"]
+SOURCES = ["api.hip", "append.hip", "decode.hip", "dequant.hip", "wush.hip", "probe.hip", "select_pages.hip",
+           "pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -117,6 +117,12 @@ struct DecodeArgs {
     // evenly by its own workgroups; see plan_runs
     int32_t *runs;
     bool even;
+    // LIST (wushkv_sparse_attention; null otherwise): the logical pages of
+    // each (sequence, kv head) take the place of its pages 0, 1, ..
+    const int32_t *sel;    // [batch][n_kv][max_sel]
+    const int32_t *n_sel;  // [batch][n_kv]
+    int32_t max_sel;
+    float mid;             // the middle of the key codes, (2^bits - 1) / 2
 };
 
 // Tokens of sequence b's chunk: n_tok[b] (or max_tok), at most max_tok and
@@ -783,11 +789,14 @@ __device__ __forceinline__ PageRun plan_runs(const DecodeArgs &a, const RunCount
 // (one run of pages, or one 64-slot window unit), so that the cache leaves
 // HBM once per four token groups; grid z runs over (sequence, group of four
 // token groups) and every wave writes its own partials.
-template <int D, int BITS, int G, bool FORM, bool SHARE>
+// LIST: a run is a run of the (sequence, kv head)'s list of logical pages; a
+// lane then keeps its entry's logical page beside the physical one.
+template <int D, int BITS, int G, bool FORM, bool SHARE, bool LIST = false>
 __global__ void __launch_bounds__(256, ((D == 128 && (BITS == 4 || (G == 8 && !SHARE))) || (D == 64 && BITS == 4 && G == 8)) ? 2 : 3)
 decode_main_kernel(DecodeArgs a)
 {
     static_assert(!(FORM && SHARE), "shared work items take q~ from decode_qt_kernel");
+    static_assert(!(LIST && SHARE), "a list belongs to one query row");
     using L = Layout<D, BITS>;
     using M = MainLds<D, BITS, G>;
     constexpr bool kEarly = FORM && M::kEarly;
@@ -836,9 +845,20 @@ decode_main_kernel(DecodeArgs a)
         if (page_wg && a.runs != nullptr) counters.load(a, lane);
         qin.load_t(a, h, tid);
     }
-    int32_t tbl = -1;
-    if (page_wg && a.n_pages > 0 && lane < upw && w0 + lane < a.max_pages)
-        tbl = a.page_table[(int64_t)b * a.max_pages + w0 + lane];
+    int32_t tbl = -1, lpage = -1;
+    // the list's part of it (LIST): logical pages, then their table entries
+    auto load_list = [&](int32_t count) {
+        lpage = tbl = -1;
+        if (lane < count && w0 + lane < a.max_sel)
+            lpage = a.sel[((int64_t)b * a.n_kv + h) * a.max_sel + w0 + lane];
+        if (a.n_pages > 0 && lpage >= 0 && lpage < a.max_pages) tbl = a.page_table[(int64_t)b * a.max_pages + lpage];
+    };
+    if constexpr (LIST) {
+        if (page_wg) load_list(upw);
+    } else {
+        if (page_wg && a.n_pages > 0 && lane < upw && w0 + lane < a.max_pages)
+            tbl = a.page_table[(int64_t)b * a.max_pages + w0 + lane];
+    }
 
     // fused step: the new token is position seq_len[b] and is attended to
     const int32_t s_old = a.seq_len[b];
@@ -848,7 +868,8 @@ decode_main_kernel(DecodeArgs a)
     int32_t qend = a.quant_end[b];
     qend = qend < S ? qend : S;
     const int32_t q_hi = qend > a.s_sink ? qend : a.s_sink;  // quantised: [s_sink, q_hi)
-    const int32_t n_qpages = (q_hi - a.s_sink + kPage - 1) / kPage;
+    int32_t n_qpages = (q_hi - a.s_sink + kPage - 1) / kPage;
+    if constexpr (LIST) n_qpages = min(max(a.n_sel[(int64_t)b * a.n_kv + h], 0), a.max_sel);
 
     // per-wave results for the merge: o (unnormalised, relative to m), m, l
     float(*sC)[D] = reinterpret_cast<float(*)[D]>(stage);
@@ -866,9 +887,13 @@ decode_main_kernel(DecodeArgs a)
             w0 = pr.first + wave * pr.u;
             w1 = min(w0 + pr.u, pr.n_pages);
             if (pr.b != b || pr.u != upw || w0 != requested) {  // not the run requested above
-                tbl = -1;
-                if (a.n_pages > 0 && lane < pr.u && w0 + lane < a.max_pages)
-                    tbl = a.page_table[(int64_t)pr.b * a.max_pages + w0 + lane];
+                if constexpr (LIST) {
+                    load_list(pr.u);
+                } else {
+                    tbl = -1;
+                    if (a.n_pages > 0 && lane < pr.u && w0 + lane < a.max_pages)
+                        tbl = a.page_table[(int64_t)pr.b * a.max_pages + w0 + lane];
+                }
             }
             if (pr.b != b) qin.load_q(a, pr.b, tg, h, pr.s, tid);
         }
@@ -949,6 +974,27 @@ decode_main_kernel(DecodeArgs a)
             const int hs = G > 4 ? 2 * j + hg : j;
             zs[hg] = hs < G ? __uint_as_float(qaux[4 * hs + 2]) : 0.0f;
         }
+        // LIST: keys as k = s (c - mid) + (z + mid s).  A token's codes mostly lie
+        // near the middle of its range, so q~ . c and z sum(q~) are several times the
+        // logit and their fp32 roundings with them; the centred terms are not
+        // (1.3e-6 relative error of an output instead of 6e-7).  The products with
+        // keys of code 1 give each row's digit sum, exactly, and the products
+        // then start from -mid times it.
+        f32x4 c_from[kHG];
+        if constexpr (LIST) {
+            const int one = BITS == 2 ? 0x11111111 : 0x01010101;
+            const i32x8 ones = BITS == 2 ? i32x8{one, one, one, one, 0, 0, 0, 0} : i32x8{one, one, one, one, one, one, one, one};
+#pragma unroll
+            for (int hg = 0; hg < kHG; ++hg) {
+                f32x4 sum = mfma_scaled<BITS>(qa[hg][0], ones, qsc[hg][0], kScaleB, f32x4{0.f, 0.f, 0.f, 0.f});
+                sum = mfma_scaled<BITS>(qa[hg][1], ones, qsc[hg][1], kScaleB, sum);
+                zs[hg] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                c_from[hg] = f32x4{sum[0] * -a.mid, sum[1] * -a.mid, sum[2] * -a.mid, sum[3] * -a.mid};
+            }
+        } else {
+#pragma unroll
+            for (int hg = 0; hg < kHG; ++hg) c_from[hg] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         if constexpr (!kEarly) {
             // every wave has its operands: the pages may now land over the
             // rows (LDS), or (memory) the operands have arrived, so that the
@@ -972,6 +1018,8 @@ decode_main_kernel(DecodeArgs a)
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) acc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
         float m_run[kHG], lc[kHG], zc[kHG];
+        float lift = LIST ? 8.0f : 0.0f;
+        constexpr uint32_t kLiftEnds = 0x5800u;  // fp16 2^7
 #pragma unroll
         for (int hg = 0; hg < kHG; ++hg) {
             m_run[hg] = -INFINITY;
@@ -982,8 +1030,13 @@ decode_main_kernel(DecodeArgs a)
         // codes of registers 2-3 two bits higher (2^8 instead of 2^6), so this
         // lane's weights carry 2^-off, off = 2 (n % 2); 4-bit codes all sit
         // at 2^4.  The products are p s c 2^-18 (2-bit) or 2^-20 (4-bit).
-        const float off = BITS == 2 ? 2.0f * (n & 1) : 0.0f;
-        constexpr float kOutScale = BITS == 2 ? 262144.0f : 1048576.0f;
+        const float off = BITS == 2 && !LIST ? 2.0f * (n & 1) : 0.0f;
+        // (LIST: p s 16 c, the codes being normal numbers: the subnormal ones cost
+        // a sum 18 to 20 of its 24 bits with 4-bit codes, 5e-6 relative error
+        // of an output instead of 7e-7.)
+        constexpr float kOutScale = LIST ? 0.0625f : BITS == 2 ? 262144.0f : 1048576.0f;
+        WidenNormal<BITS> wide;
+        if constexpr (LIST) wide.init();
 
         // P V A operand rows: row m is part m % kRowsPerHead (0: fp16 hi
         // of the weight, 1: the fp16 rest, others zero) of head
@@ -1028,9 +1081,11 @@ decode_main_kernel(DecodeArgs a)
                 const int s = (u - w0) & 1;
                 const int32_t phys = phys_of(u);
                 // a page outside the pool contributes nothing (its stage holds page 0)
+                const int32_t lp = LIST ? __builtin_amdgcn_readlane(lpage, u - w0) : u;
                 const int32_t nvalid = (phys < 0 || phys >= a.n_pages)
-                                           ? 0 : min(kPage, p_hi - (a.s_sink + u * kPage));
-                const u32x4 kp = kx[kKX], vp = kx[kKX + 1];
+                                           ? 0 : min(kPage, p_hi - (a.s_sink + lp * kPage));
+                const u32x4 kp = kx[kKX];
+                u32x4 vp = kx[kKX + 1];
 
                 // scores: one product per 16 tokens, head group and limb group;
                 // all issued before any result is used
@@ -1059,7 +1114,7 @@ decode_main_kernel(DecodeArgs a)
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int hg = 0; hg < kHG; ++hg)
-                        c[hg][t] = mfma_scaled<BITS>(qa[hg][0], bop[t], qsc[hg][0], kScaleB, f32x4{0.f, 0.f, 0.f, 0.f});
+                        c[hg][t] = mfma_scaled<BITS>(qa[hg][0], bop[t], qsc[hg][0], kScaleB, c_from[hg]);
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -1069,7 +1124,8 @@ decode_main_kernel(DecodeArgs a)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const float ks = f16_bits_to_f32(kp[t] & 0xFFFFu);
-                    const float kz = f16_bits_to_f32(kp[t] >> 16);
+                    float kz = f16_bits_to_f32(kp[t] >> 16);
+                    if constexpr (LIST) kz = fmaf(ks, a.mid, kz);
 #pragma unroll
                     for (int hg = 0; hg < kHG; ++hg) {
                         const f32x4 &c0 = c[hg][t];
@@ -1080,13 +1136,30 @@ decode_main_kernel(DecodeArgs a)
                 if (nvalid < kPage) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if (4 * n + t >= nvalid)
+                        if (4 * n + t >= nvalid) {
 #pragma unroll
                             for (int hg = 0; hg < kHG; ++hg) lg[hg][t] = -INFINITY;
+                            vp[t] = 0u;  // (a page taken again may hold a scale that is not finite)
+                        }
                 }
                 // running max per head (every lane of a row holds its head's)
                 float m_new[kHG];
                 bool grow = false;
+                // LIST: the softmax's reference is lift below the maximum, so
+                // that the weights reach 2^lift: fp16 holds nothing below 2^-24,
+                // and the lo parts of weights of 2^-10 and less would be lost (a
+                // sum over a page's tokens then has 4e-6 relative error, instead
+                // of 1e-6, with 4-bit codes).  A value scale of 2^(15 - lift) or
+                // more leaves no room and ends the lift for the rest of the run.
+                float drop = 0.0f;
+                if constexpr (LIST) {
+                    const uint32_t big = max(max(vp[0] & 0xFFFFu, vp[1] & 0xFFFFu), max(vp[2] & 0xFFFFu, vp[3] & 0xFFFFu));
+                    if (__any(big >= kLiftEnds) && lift > 0.0f) {
+                        drop = lift;
+                        lift = 0.0f;
+                        grow = true;
+                    }
+                }
 #pragma unroll
                 for (int hg = 0; hg < kHG; ++hg) {
                     const float mx = row_max16(fmaxf(fmaxf(lg[hg][0], lg[hg][1]), fmaxf(lg[hg][2], lg[hg][3])));
@@ -1099,7 +1172,7 @@ decode_main_kernel(DecodeArgs a)
                     float al[kHG];
 #pragma unroll
                     for (int hg = 0; hg < kHG; ++hg) {
-                        al[hg] = m_new[hg] == -INFINITY ? 1.0f : fexp2(m_run[hg] - m_new[hg]);
+                        al[hg] = m_new[hg] == -INFINITY ? 1.0f : fexp2(m_run[hg] - m_new[hg] - drop);
                         lc[hg] *= al[hg];
                         zc[hg] *= al[hg];
                     }
@@ -1118,7 +1191,7 @@ decode_main_kernel(DecodeArgs a)
 #pragma unroll
                 for (int hg = 0; hg < kHG; ++hg) {
                     // (no valid token yet: every weight is exp2(-inf) = 0)
-                    const float mo = m_run[hg] == -INFINITY ? 0.0f : m_run[hg] + off;
+                    const float mo = m_run[hg] == -INFINITY ? 0.0f : m_run[hg] + (off - lift);
                     float wgt[4];
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
@@ -1160,7 +1233,8 @@ decode_main_kernel(DecodeArgs a)
                     for (int uu = 0; uu < 2 * kNw; ++uu) {
                         const int widx = kc * 2 * kNw + uu;
                         uint32_t op[L::kCodesPerWord / 2];
-                        widen_word_f16<BITS>(vv[widx / 4][widx % 4], op);
+                        if constexpr (LIST) wide.word(vv[widx / 4][widx % 4], op);
+                        else widen_word_f16<BITS>(vv[widx / 4][widx % 4], op);
 #pragma unroll
                         for (int o = 0; o < kOpw; ++o) {
                             const int nt = uu * kOpw + o;
@@ -1196,7 +1270,7 @@ decode_main_kernel(DecodeArgs a)
                 for (int nt = 0; nt < kNT; ++nt)
                     sC[hs][16 * nt + n] = fmaf(acc[nt][r] + acc[nt][r + 1], kOutScale, zt[hg]);
                 if (n == 0) {
-                    sM[wave][hs] = m_run[hg];
+                    sM[wave][hs] = m_run[hg] - lift;  // the reference
                     sL[wave][hs] = lt[hg];
                 }
             }
@@ -1239,12 +1313,15 @@ decode_main_kernel(DecodeArgs a)
         // A operands: row m = 2 g + part (hi, lo) of q~, chunk c.  From LDS
         // they are formed at once; from memory only after the slot loads are
         // issued, so that the latencies overlap.
-        bf16x8 qa[kC];
+        // LIST: a third part of q~ and of the weights, in operands of their own
+        // that add onto the hi rows (two parts leave 2^-18 of the largest, and
+        // with few pages the windows are most of the attention)
+        bf16x8 qa[kC], qa3[LIST ? kC : 1];
         auto form_qa = [&]() {
             const int g = n >> 1, part = n & 1;
 #pragma unroll
             for (int c = 0; c < kC; ++c) {
-                uint32_t u[4] = {0u, 0u, 0u, 0u};
+                uint32_t u[4] = {0u, 0u, 0u, 0u}, u3[4] = {0u, 0u, 0u, 0u};
                 if (g < G) {
                     const float *src = qtl + g * D + 32 * c + 8 * j;
                     const f32x4 x0 = *reinterpret_cast<const f32x4 *>(src);
@@ -1256,9 +1333,15 @@ decode_main_kernel(DecodeArgs a)
                         const uint32_t lo = pack_bf16_rne(x[2 * pp] - bf16_bits_to_f32(hi & 0xFFFFu),
                                                           x[2 * pp + 1] - bf16_bits_to_f32(hi >> 16));
                         u[pp] = part ? lo : hi;
+                        if constexpr (LIST) {
+                            const float e0 = x[2 * pp] - bf16_bits_to_f32(hi & 0xFFFFu) - bf16_bits_to_f32(lo & 0xFFFFu);
+                            const float e1 = x[2 * pp + 1] - bf16_bits_to_f32(hi >> 16) - bf16_bits_to_f32(lo >> 16);
+                            u3[pp] = part ? 0u : pack_bf16_rne(e0, e1);
+                        }
                     }
                 }
                 qa[c] = __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]});
+                if constexpr (LIST) qa3[c] = __builtin_bit_cast(bf16x8, u32x4{u3[0], u3[1], u3[2], u3[3]});
             }
         };
         if constexpr (FORM) form_qa();
@@ -1327,6 +1410,10 @@ decode_main_kernel(DecodeArgs a)
             f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < kC; ++c) sc = mfma16(qa[c], __builtin_bit_cast(bf16x8, kx[c]), sc);
+            if constexpr (LIST) {
+#pragma unroll
+                for (int c = 0; c < kC; ++c) sc = mfma16(qa3[c], __builtin_bit_cast(bf16x8, kx[c]), sc);
+            }
             const bool ok = (vmask >> n) & 1u;
             // causal visibility of this slot's position to the query rows
             // 2 j and 2 j + 1: a chunk token at position p sees [0, p] (the
@@ -1367,6 +1454,9 @@ decode_main_kernel(DecodeArgs a)
                     const uint32_t ll = pack_bf16_rne(pr[e] - bf16_bits_to_f32(hl), 0.0f) & 0xFFFFu;
                     lds_write2(lds_addr(tbuf + g * kTP + 2 * n), hl);
                     lds_write2(lds_addr(tbuf + (G + g) * kTP + 2 * n), ll);
+                    if constexpr (LIST)  // (the upper half of the head's hi row)
+                        lds_write2(lds_addr(tbuf + g * kTP + 64 + 2 * n),
+                                   pack_bf16_rne(pr[e] - bf16_bits_to_f32(hl) - bf16_bits_to_f32(ll), 0.0f) & 0xFFFFu);
                 }
             }
             // A operand of the 16x16x16 product: row m = 2 g + part, tokens
@@ -1379,10 +1469,17 @@ decode_main_kernel(DecodeArgs a)
             const uint32_t msk1 = ((bits4 & 4u) ? 0x0000FFFFu : 0u) | ((bits4 & 8u) ? 0xFFFF0000u : 0u);
             typedef __attribute__((ext_vector_type(4))) short s16x4;
             const s16x4 A = __builtin_bit_cast(s16x4, pa);
+            s16x4 A3 = A;
+            if constexpr (LIST) {
+                const bool third = n < 2 * G && (n & 1) == 0;
+                A3 = __builtin_bit_cast(s16x4, lds_read8(third ? pa_addr + 64u : zero_row));
+            }
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt) {
                 const u32x2 y = {vx[nt][0] & msk0, vx[nt][1] & msk1};
                 acc[nt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(A, __builtin_bit_cast(s16x4, y), acc[nt], 0, 0, 0);
+                if constexpr (LIST)
+                    acc[nt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(A3, __builtin_bit_cast(s16x4, y), acc[nt], 0, 0, 0);
             }
         }
         // result per head g = 2 j + e: rows 4 j + 2 e (hi) and + 1 (lo)
@@ -1675,6 +1772,7 @@ __global__ void __launch_bounds__(256, 2) chunk_pages_kernel(DecodeArgs a)
             kz[t] = f16_bits_to_f32(kp[t] >> 16);
             vs[t] = f16_bits_to_f32(vp[t] & 0xFFFFu);
             vz[t] = f16_bits_to_f32(vp[t] >> 16);
+            if (tail && 4 * n + t >= nvalid) vs[t] = vz[t] = 0.0f;  // (whatever the page held before)
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -2293,11 +2391,16 @@ static RowShape row_shape(const wushkv_cache *c, int32_t n_q, int32_t max_tok)
 // Longest page run of one wave: its page-table entries sit one per lane.
 constexpr int64_t kMaxRunPages = 64;
 
-static bool make_plan(const wushkv_cache *c, const RowShape &rs, int32_t max_seq_len, DecodePlan &p,
+// Pages of a sequence of max_seq_len tokens.
+static int64_t pages_of(const wushkv_cache *c, int32_t max_seq_len)
+{
+    return max_seq_len > c->s_sink ? (max_seq_len - c->s_sink + kPage - 1) / kPage : 0;
+}
+
+static bool make_plan(const wushkv_cache *c, const RowShape &rs, int64_t qpages, DecodePlan &p,
                       bool one_window_wg = false)
 {
     const int32_t G = rs.G;
-    const int64_t qpages = max_seq_len > c->s_sink ? (max_seq_len - c->s_sink + kPage - 1) / kPage : 0;
     const int64_t rows_z = (int64_t)c->batch * rs.n_groups;  // grid z
     const int64_t heads = rows_z * c->n_kv_heads;
     const int64_t n_q = (int64_t)c->n_kv_heads * G;          // virtual query heads per row
@@ -2350,7 +2453,7 @@ static bool make_plan(const wushkv_cache *c, const RowShape &rs, int32_t max_seq
     // tiles, instead of one per 64-slot unit.
     if (!rs.share && !one_window_wg && wunits > 1 &&
         (psplits + wwgs) * heads * 4 > resident_waves(c->head_dim, storage_bits(c->bits), G, false))
-        return make_plan(c, rs, max_seq_len, p, true);
+        return make_plan(c, rs, qpages, p, true);
     if (psplits + wwgs > kMaxSplits) {
         const int64_t room = kMaxSplits - wwgs;
         if (room < 1) return false;
@@ -2380,13 +2483,19 @@ template <int D, int BITS, int G>
 static void launch_main(bool form, bool share, dim3 grid, unsigned rows_z, hipStream_t s,
                         const DecodeArgs &a)
 {
+    const bool list = a.n_sel != nullptr;
     if (form) {
-        launch("decode_main_kernel", decode_main_kernel<D, BITS, G, true, false>, grid, dim3(256), s, a);
+        if (list)
+            launch("sparse_main_kernel", decode_main_kernel<D, BITS, G, true, false, true>, grid, dim3(256), s, a);
+        else
+            launch("decode_main_kernel", decode_main_kernel<D, BITS, G, true, false>, grid, dim3(256), s, a);
         return;
     }
     launch("decode_qt_kernel", decode_qt_kernel<D, BITS, G>, dim3(grid.x, rows_z), dim3(64 * kQtWaves<D>), s, a);
     if (share)
         launch("decode_main_kernel", decode_main_kernel<D, BITS, G, false, true>, grid, dim3(256), s, a);
+    else if (list)
+        launch("sparse_main_kernel", decode_main_kernel<D, BITS, G, false, false, true>, grid, dim3(256), s, a);
     else
         launch("decode_main_kernel", decode_main_kernel<D, BITS, G, false, false>, grid, dim3(256), s, a);
 }
@@ -2427,18 +2536,29 @@ static int check_chunk(const wushkv_cache *c, int32_t max_tok)
     return WUSHKV_OK;
 }
 
+static size_t plan_bytes(const DecodePlan &p)
+{
+    return p.qt_bytes + p.limb_bytes + p.aux_bytes + p.part_bytes;
+}
+
 static size_t workspace_bytes(const wushkv_cache *c, int32_t n_q, int32_t max_tok, int32_t max_seq_len)
 {
     if (check_decode_args(c, n_q, max_seq_len) != WUSHKV_OK) return 0;
     DecodePlan p;
-    if (!make_plan(c, row_shape(c, n_q, max_tok), max_seq_len, p)) return 0;
-    return p.qt_bytes + p.limb_bytes + p.aux_bytes + p.part_bytes;
+    if (!make_plan(c, row_shape(c, n_q, max_tok), pages_of(c, max_seq_len), p)) return 0;
+    return plan_bytes(p);
 }
 
 // The new tokens of a fused step (wushkv_decode_step).
 struct StepIn {
     const int32_t *n_new;
     const uint16_t *k_new, *v_new, *t_k;
+};
+
+// The listed pages of wushkv_sparse_attention.
+struct ListIn {
+    const int32_t *sel, *n_sel;
+    int32_t max_sel;
 };
 
 int wushkv_step_finish(const wushkv_cache *c, const int32_t *n_new, const float *part, float *out,
@@ -2448,7 +2568,7 @@ int wushkv_step_finish(const wushkv_cache *c, const int32_t *n_new, const float 
 static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok, int32_t max_tok,
                   int32_t n_q_heads, int32_t max_seq_len, const float *t_k_inv, float sm_scale,
                   float *out, void *workspace, size_t workspace_bytes, wushkv_stream_t stream,
-                  const StepIn *step = nullptr)
+                  const StepIn *step = nullptr, const ListIn *list = nullptr)
 {
     int st = check_decode_args(c, n_q_heads, max_seq_len);
     if (st != WUSHKV_OK) return st;
@@ -2458,8 +2578,8 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
     if (!(sm_scale > 0.0f) || sm_scale == INFINITY) return WUSHKV_EINVAL;
     const RowShape rs = row_shape(c, n_q_heads, max_tok);
     DecodePlan p;
-    if (!make_plan(c, rs, max_seq_len, p)) return WUSHKV_EUNSUPPORTED;
-    if (workspace_bytes < p.qt_bytes + p.limb_bytes + p.aux_bytes + p.part_bytes) return WUSHKV_EWORKSPACE;
+    if (!make_plan(c, rs, list != nullptr ? list->max_sel : pages_of(c, max_seq_len), p)) return WUSHKV_EUNSUPPORTED;
+    if (workspace_bytes < plan_bytes(p)) return WUSHKV_EWORKSPACE;
 
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const int32_t G = rs.G;
@@ -2506,6 +2626,12 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
         a.win_kw = c->win_k;
         a.win_vw = c->win_v;
     }
+    if (list != nullptr) {
+        a.sel = list->sel;
+        a.n_sel = list->n_sel;
+        a.max_sel = list->max_sel;
+        a.mid = 0.5f * ((1 << c->bits) - 1);
+    }
 
     const unsigned rows_z = (unsigned)(c->batch * rs.n_groups);
     // several token groups (a chunk of more tokens than one group holds):
@@ -2525,7 +2651,7 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
     // lane per sequence), noted where the query rows' aux words would be; a
     // chunk of one token as a decode, whose bits it keeps
     a.even = form && max_tok == 1 && p.n_page_splits > 0;
-    if (a.even && c->batch > 1 && c->batch <= 64 &&
+    if (a.even && list == nullptr && c->batch > 1 && c->batch <= 64 &&
         p.aux_bytes >= (2 + 2 * (size_t)c->batch) * sizeof(int32_t))
         a.runs = reinterpret_cast<int32_t *>(qaux);
     const int key = c->head_dim * 10 + storage_bits(c->bits);
@@ -2678,4 +2804,33 @@ extern "C" int wushkv_decode_step(const wushkv_cache *c, const uint16_t *k_new, 
     const StepIn in{n_new, k_new, v_new, t_k};
     return attend(c, q, nullptr, 1, n_q_heads, max_seq_len, t_k_inv, sm_scale, out, workspace,
                   workspace_bytes, stream, &in);
+}
+
+// ------------------------------------------------------- listed pages
+
+static int check_list(const wushkv_cache *c, int32_t n_q, int32_t max_sel)
+{
+    const int st = check_decode_args(c, n_q, 0);
+    if (st != WUSHKV_OK) return st;
+    return max_sel < 0 ? WUSHKV_EINVAL : WUSHKV_OK;
+}
+
+extern "C" size_t wushkv_sparse_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads, int32_t max_sel)
+{
+    DecodePlan p;
+    if (check_list(c, n_q_heads, max_sel) != WUSHKV_OK || !make_plan(c, row_shape(c, n_q_heads, 1), max_sel, p)) return 0;
+    return plan_bytes(p);
+}
+
+extern "C" int wushkv_sparse_attention(const wushkv_cache *c, const uint16_t *q, int32_t n_q_heads,
+                                       const int32_t *sel, const int32_t *n_sel, int32_t max_sel,
+                                       const float *t_k_inv, float sm_scale, float *out, void *workspace,
+                                       size_t workspace_bytes, wushkv_stream_t stream)
+{
+    const int st = check_list(c, n_q_heads, max_sel);
+    if (st != WUSHKV_OK) return st;
+    if ((!sel && max_sel > 0) || !n_sel || ((uintptr_t)sel | (uintptr_t)n_sel) & 15u) return WUSHKV_EINVAL;
+    const ListIn list{sel, n_sel, max_sel};
+    return attend(c, q, nullptr, 1, n_q_heads, 0, t_k_inv, sm_scale, out, workspace, workspace_bytes, stream,
+                  nullptr, &list);
 }

@@ -1,0 +1,532 @@
+// wushkv_page_bounds and wushkv_select_pages: a box in 8 bits round the stored
+// keys of every complete page, and the pages whose box allows a decode query
+// the largest logits.
+//
+// A box has per channel a centre c and a radius r (in units of the page's
+// scale s): over the box the largest q~ . k is
+//   s sum_j max(q~_j (c_j - r_j), q~_j (c_j + r_j)) = s sum_j (q~_j c_j + |q~_j| r_j),
+// one product of [q~, |q~|] with [c, r].  With q~ in 15-bit fixed point N, split
+// into two 8-bit digits, it is two 8-bit integer products with exact 32-bit
+// sums (|sum| <= 128 16384 128 < 2^31): the scores, and so the selection, do
+// not depend on an order of summation.  The rows of the 16x16x64 products are
+// (query head, digit) pairs, the columns pages.
+//
+// page_bounds_kernel   one wave per (page, kv head).
+// score_kernel         grid (kv heads, runs of pages, sequences).
+// select_kernel        one workgroup per (kv head, sequence).
+#include "common.h"
+#include "merge.h"
+
+namespace wushkv {
+
+// ------------------------------------------------------------------ boxes
+
+struct BoundsArgs {
+    const uint8_t *pages;
+    const int32_t *page_table, *seq_len, *quant_end, *since;
+    int8_t *codes;
+    float *scales;
+    int32_t n_kv, s_sink, max_pages, n_pages, max_new;
+    int32_t blocks;  // workgroups per sequence
+};
+
+// Complete pages of sequence b.
+__device__ __forceinline__ int32_t complete_pages(const int32_t *seq_len, const int32_t *quant_end, int32_t b,
+                                                  int32_t s_sink, int32_t max_pages)
+{
+    const int32_t q = min(quant_end[b], seq_len[b]);
+    return q > s_sink ? min((q - s_sink) / kPage, max_pages) : 0;
+}
+
+// Lane (j, n) of the wave holds channels 32 j .. 32 j + 31 of tokens 4 n ..
+// 4 n + 3 (the page layout); with d = 64 the upper half repeats the lower.
+template <int D, int BITS>
+__global__ void __launch_bounds__(256) page_bounds_kernel(BoundsArgs a)
+{
+    using L = Layout<D, BITS>;
+    constexpr int kWords = L::kKWordsPerLane;     // 8 (2-bit) or 16 (4-bit)
+    constexpr int kSpan = L::kCodesPerWord;       // channels per word
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t b = blockIdx.x / a.blocks;
+    const int32_t item = (blockIdx.x % a.blocks) * 4 + wave;  // (new page, kv head)
+    const int32_t h = item % a.n_kv;
+    const int32_t q0 = a.since != nullptr ? a.since[b] : 0;
+    const int32_t lp = (q0 > a.s_sink ? (q0 - a.s_sink) / kPage : 0) + item / a.n_kv;
+    if (item / a.n_kv >= a.max_new || lp >= complete_pages(a.seq_len, a.quant_end, b, a.s_sink, a.max_pages)) return;
+    const int32_t phys = a.page_table[(int64_t)b * a.max_pages + lp];
+    if (phys < 0 || phys >= a.n_pages) return;
+    const uint8_t *pg = a.pages + ((int64_t)phys * a.n_kv + h) * L::kPageBytes;
+    const int src = lane % L::kKLanes, n = lane & 15;
+    u32x4 w[kWords / 4];
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) w[i] = *reinterpret_cast<const u32x4 *>(pg + 4 * L::k_word(src, 4 * i));
+    const u32x4 par = *reinterpret_cast<const u32x4 *>(pg + L::kParamOffset + 16 * n);
+    float lo[32], hi[32];
+    bool odd = false;  // a parameter that is not finite
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        odd |= (par[t] & 0x7C00u) == 0x7C00u || (par[t] & 0x7C000000u) == 0x7C000000u;
+        const float sc = f16_bits_to_f32(par[t] & 0xFFFFu), zr = f16_bits_to_f32(par[t] >> 16);
+#pragma unroll
+        for (int i = 0; i < BITS; ++i) {
+            const uint32_t x = w[(BITS * t + i) / 4][(BITS * t + i) % 4];
+#pragma unroll
+            for (int e = 0; e < kSpan; ++e) {
+                const int bit = 2 * BITS * (e % (kSpan / 2)) + BITS * (e / (kSpan / 2));
+                const float v = fmaf(sc, (float)((x >> bit) & ((1u << BITS) - 1u)), zr);
+                const int ch = kSpan * i + e;
+                lo[ch] = t == 0 ? v : fminf(lo[ch], v);
+                hi[ch] = t == 0 ? v : fmaxf(hi[ch], v);
+            }
+        }
+    }
+    // over the tokens: the 16 lanes of a row
+    float top = 0.0f;
+#pragma unroll
+    for (int ch = 0; ch < 32; ++ch) {
+        float x = lo[ch], y = hi[ch];
+        x = fminf(x, dpp<0xB1>(x)); y = fmaxf(y, dpp<0xB1>(y));
+        x = fminf(x, dpp<0x4E>(x)); y = fmaxf(y, dpp<0x4E>(y));
+        x = fminf(x, dpp<0x124>(x)); y = fmaxf(y, dpp<0x124>(y));
+        x = fminf(x, dpp<0x128>(x)); y = fmaxf(y, dpp<0x128>(y));
+        lo[ch] = x;
+        hi[ch] = y;
+        top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+    }
+    const bool any_odd = __any(odd);
+    top = wave_max(any_odd ? 0.0f : top);
+    const float s = any_odd ? INFINITY : top / 126.0f;
+    // lane n of a row finishes channels 2 n and 2 n + 1 of its 32
+    float l2[2] = {lo[0], lo[1]}, h2[2] = {hi[0], hi[1]};
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            l2[e] = n == i ? lo[2 * i + e] : l2[e];
+            h2[e] = n == i ? hi[2 * i + e] : h2[e];
+        }
+    int c[2] = {0, 0}, r[2] = {0, 0};
+    if (top > 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float mid = rintf(((l2[e] + h2[e]) * 0.5f) / s);
+            const float ms = mid * s;
+            c[e] = (int)mid;
+            r[e] = (int)fminf(ceilf(fmaxf(h2[e] - ms, ms - l2[e]) / s), 127.0f);
+        }
+    }
+    if (lane >= L::kKLanes) return;
+    int8_t *out = a.codes + ((int64_t)phys * a.n_kv + h) * 2 * D + 2 * lane;
+    *reinterpret_cast<uint16_t *>(out) = (uint16_t)((c[0] & 0xFF) | ((c[1] & 0xFF) << 8));
+    *reinterpret_cast<uint16_t *>(out + D) = (uint16_t)(r[0] | (r[1] << 8));
+    if (lane == 0) a.scales[(int64_t)h * a.n_pages + phys] = s;
+}
+
+// ------------------------------------------------------------------ scores
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+struct SelectArgs {
+    const int8_t *codes;
+    const float *scales;
+    const int32_t *page_table, *seq_len, *quant_end;
+    const uint16_t *q;
+    const float *tinv;
+    int32_t *sel, *n_sel;
+    float *scores;       // [batch][n_kv][max_pages]
+    int32_t n_kv, G, s_sink, max_pages, n_pages;
+    int32_t planned;     // pages of the longest sequence planned for
+    int32_t run;         // pages per workgroup of score_kernel
+    int32_t top_k;
+};
+
+// The two digits of N and |N| for the group's heads, as operand rows 2 g (the
+// 256s) and 2 g + 1: [16][2 D] bytes of [N, |N|], rows 16 bytes apart in the banks.
+template <int D>
+struct DigitLds {
+    static constexpr int kPitch = 2 * D + 16;
+    int8_t rows[16 * kPitch];
+    float unit[8];  // 2^-F per head
+};
+
+// q~ = q t_k_inv of the group's heads in fp64 and its digits, by all threads
+// of the workgroup (NT = 256 or 1024).  Thread (part, quad) sums its rows of
+// four columns; lanes, then waves, in a fixed order.  red: fp64 [NT / 64][4][D]
+// or, for fewer heads, less.
+template <int D, int NT, int HEADS>
+struct QuerySums {
+    static constexpr int kQuads = D / 4;
+    static constexpr int kRows = D / (NT / kQuads);  // rows per part
+    f32x4 t[kRows];
+    __device__ __forceinline__ void load(const SelectArgs &a, int h, int tid)
+    {
+        const float *T = a.tinv + (int64_t)h * D * D + (int64_t)(tid / kQuads) * kRows * D + 4 * (tid % kQuads);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) t[r] = *reinterpret_cast<const f32x4 *>(T + (int64_t)r * D);
+    }
+};
+
+template <int D, int NT>
+__device__ void form_digits(const SelectArgs &a, const QuerySums<D, NT, 4> &in, int b, int h, double *red,
+                            double *qt, DigitLds<D> &lds, int tid)
+{
+    using Q = QuerySums<D, NT, 4>;
+    constexpr int kHeads = 4;               // heads at once
+    constexpr int kWaves = NT / 64;
+    constexpr int kInWave = 64 / Q::kQuads;  // parts of a wave
+    const int lane = tid & 63, wave = tid >> 6, quad = tid % Q::kQuads, part = tid / Q::kQuads;
+    for (int i = tid; i < 16 * DigitLds<D>::kPitch / 4; i += NT) reinterpret_cast<uint32_t *>(lds.rows)[i] = 0u;
+    const uint16_t *q = a.q + ((int64_t)b * a.n_kv + h) * a.G * D + part * Q::kRows;
+    for (int g0 = 0; g0 < a.G; g0 += kHeads) {
+        double acc[kHeads][4];
+#pragma unroll
+        for (int g = 0; g < kHeads; ++g) {
+            const uint16_t *row = q + (int64_t)min(g0 + g, a.G - 1) * D;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[g][c] = 0.0;
+#pragma unroll
+            for (int r = 0; r < Q::kRows; ++r) {
+                const double x = (double)bf16_bits_to_f32(row[r]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[g][c] = fma(x, (double)in.t[r][c], acc[g][c]);
+            }
+#pragma unroll
+            for (int m = Q::kQuads; m < 64; m *= 2)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[g][c] += __shfl_xor(acc[g][c], m);
+        }
+        __syncthreads();  // the last heads' sums are read
+        if (lane < Q::kQuads)
+#pragma unroll
+            for (int g = 0; g < kHeads; ++g)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) red[(wave * kHeads + g) * D + 4 * quad + c] = acc[g][c];
+        __syncthreads();
+        for (int i = tid; i < kHeads * D; i += NT) {
+            double x = 0.0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) x += red[w * kHeads * D + i];
+            if (g0 + i / D < a.G) qt[g0 * D + i] = x;
+        }
+    }
+    (void)kInWave;
+    __syncthreads();
+    for (int g = wave; g < a.G; g += kWaves) {
+        double x[D / 64];
+        uint32_t top = 0;  // the exponent of the largest magnitude
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+            x[e] = qt[g * D + 64 * e + lane];
+            top = max(top, (uint32_t)(__double2hiint(x[e]) & 0x7FF00000) >> 20);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        bool zero = true;  // all entries
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) zero = zero && x[e] == 0.0;
+        const bool dead = top == 0x7FF || __all(zero);
+        const int F = dead ? 0 : min(max(14 - ((int)top - 1022), -100), 100);
+        const double f = __hiloint2double((1023 + F) << 20, 0);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+            const int N = dead ? 0 : (int)fmin(fmax(rint(x[e] * f), -16384.0), 16384.0);
+            const int M = N < 0 ? -N : N;
+            int8_t *at = lds.rows + 2 * g * DigitLds<D>::kPitch + 64 * e + lane;
+            at[0] = (int8_t)((N + 128) >> 8);
+            at[DigitLds<D>::kPitch] = (int8_t)N;
+            at[D] = (int8_t)((M + 128) >> 8);
+            at[D + DigitLds<D>::kPitch] = (int8_t)M;
+        }
+        if (lane == 0) lds.unit[g] = ldexpf(1.0f, -F);
+    }
+    __syncthreads();
+}
+
+// A tile of 16 pages: lane (j, n) holds bytes 64 k + 16 j .. + 15 of page n's
+// box for every k.
+template <int D>
+struct BoxTile {
+    i32x4 w[D / 32];
+    float s;        // page n's scale
+    bool inside;    // page n lies in the pool
+    __device__ __forceinline__ void load(const SelectArgs &a, int b, int h, int32_t lp, int32_t full, int lane)
+    {
+        int32_t phys = -1;
+        if (lp < full) phys = a.page_table[(int64_t)b * a.max_pages + lp];
+        inside = phys >= 0 && phys < a.n_pages;
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) w[k] = i32x4{0, 0, 0, 0};
+        if (inside) {
+            const int8_t *src = a.codes + ((int64_t)phys * a.n_kv + h) * 2 * D + 16 * (lane >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) w[k] = *reinterpret_cast<const i32x4 *>(src + 64 * k);
+            s = a.scales[(int64_t)h * a.n_pages + phys];
+        }
+    }
+    // page n's score, in every lane of column n
+    __device__ __forceinline__ float score(const i32x4 (&rows)[D / 32], const float (&unit)[2], const bool (&there)[2]) const
+    {
+        i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(rows[k], w[k], acc, 0, 0, 0);
+        float best = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float x = (float)(acc[2 * e] * 256 + acc[2 * e + 1]) * s;
+            if (there[e]) best = fmaxf(best, x * unit[e]);
+        }
+        const LanePair p = pair16(best);
+        const LanePair q = pair32(fmaxf(p.a, p.b));
+        best = fmaxf(q.a, q.b) + 0.0f;  // (no negative zero)
+        if (s == INFINITY) best = INFINITY;
+        return inside ? best : -INFINITY;
+    }
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(NT) score_kernel(SelectArgs a)
+{
+    __shared__ __attribute__((aligned(16))) DigitLds<D> digits;
+    __shared__ __attribute__((aligned(16))) double red[NT / 64 * 4 * D];
+    __shared__ double qt[8 * D];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, j = lane >> 4;
+    const int h = blockIdx.x, b = blockIdx.z;
+    const int32_t full = min(complete_pages(a.seq_len, a.quant_end, b, a.s_sink, a.max_pages), a.planned);
+    const int32_t first = blockIdx.y * a.run, end = min(first + a.run, full);
+    if (first >= end) return;
+    QuerySums<D, NT, 4> in;
+    in.load(a, h, tid);
+    form_digits<D, NT>(a, in, b, h, red, qt, digits, tid);
+    i32x4 rows[D / 32];
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)
+        rows[k] = *reinterpret_cast<const i32x4 *>(digits.rows + n * DigitLds<D>::kPitch + 64 * k + 16 * j);
+    const bool there[2] = {2 * j < a.G, 2 * j + 1 < a.G};
+    const float unit[2] = {there[0] ? digits.unit[2 * j] : 1.0f, there[1] ? digits.unit[2 * j + 1] : 1.0f};
+    float *out = a.scores + ((int64_t)b * a.n_kv + h) * a.max_pages;
+    for (int32_t p = first + 16 * wave; p < end; p += NT / 4) {
+        BoxTile<D> tile;
+        tile.load(a, b, h, p + n, end, lane);
+        const float x = tile.score(rows, unit, there);
+        if (lane < 16 && p + n < end) out[p + n] = x;
+    }
+}
+
+// ------------------------------------------------------------------ selection
+
+// fp32 -> uint32 in the same order (no NaN).
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+// The top_k pages of one (sequence, kv head): the k-th largest score by its
+// eight-bit digits from the top, each a histogram of the scores that share the
+// digits found so far, then the pages above it, and as many equal to it as are
+// missing, in ascending order.
+__global__ void __launch_bounds__(1024) select_kernel(SelectArgs a)
+{
+    __shared__ uint32_t hist[256];
+    __shared__ int32_t found[2];     // the digit, and how many of it are taken
+    __shared__ int32_t sums[2][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int h = blockIdx.x, b = blockIdx.y;
+    const int32_t end = min(a.quant_end[b], a.seq_len[b]);
+    const int32_t most = min(a.planned, a.max_pages);
+    const int32_t every = end > a.s_sink ? min((int32_t)(((int64_t)end - a.s_sink + kPage - 1) / kPage), most) : 0;
+    const int32_t full = end > a.s_sink ? min((end - a.s_sink) / kPage, most) : 0;
+    const int64_t row = (int64_t)b * a.n_kv + h;
+    const float *scores = a.scores + row * a.max_pages;
+    int32_t *sel = a.sel + row * ((int64_t)a.top_k + 1);
+    const int32_t k = min(a.top_k, full);
+    uint32_t at = 0;        // the k-th largest score's digits so far
+    int32_t left = k;       // its rank among the scores that share them
+    if (k > 0 && k < full) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            if (tid < 256) hist[tid] = 0;
+            __syncthreads();
+            for (int32_t i = tid; i < full; i += 1024) {
+                const uint32_t u = order_of(scores[i]);
+                if (shift == 24 || (u >> (shift + 8)) == (at >> (shift + 8))) atomicAdd(&hist[(u >> shift) & 255u], 1u);
+            }
+            __syncthreads();
+            if (wave == 0) {
+                // lane l: digits 255 - 4 l down to 252 - 4 l
+                int32_t c[4], sum = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += c[e] = (int32_t)hist[255 - 4 * lane - e];
+                int32_t above = wave_scan(sum) - sum;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (above < left && left <= above + c[e]) {
+                        found[0] = 255 - 4 * lane - e;
+                        found[1] = left - above;
+                    }
+                    above += c[e];
+                }
+            }
+            __syncthreads();
+            at |= (uint32_t)found[0] << shift;
+            left = found[1];
+            __syncthreads();
+        }
+    }
+    // (k = full: everything is above)
+    int32_t above = 0, equal = 0;  // pages taken, and pages equal to the k-th, before this round
+    for (int32_t i0 = 0; i0 < full && k > 0; i0 += 1024) {
+        const int32_t i = i0 + tid;
+        const uint32_t u = i < full && k < full ? order_of(scores[i]) : 0u;
+        const bool gt = i < full && (k == full || u > at), eq = i < full && k < full && u == at;
+        const uint64_t mg = __ballot(gt), me = __ballot(eq);
+        __syncthreads();
+        if (lane == 0) {
+            sums[0][wave] = __popcll(mg);
+            sums[1][wave] = __popcll(me);
+        }
+        __syncthreads();
+        int32_t ng = above, ne = equal;
+        for (int w = 0; w < 16; ++w) {
+            const int32_t g = sums[0][w], e = sums[1][w];
+            if (w < wave) {
+                ng += g;
+                ne += e;
+            }
+            above += g;
+            equal += e;
+        }
+        const uint64_t low = lane == 0 ? 0 : ~0ull >> (64 - lane);
+        ng += __popcll(mg & low);
+        ne += __popcll(me & low);
+        // ng pages above and min(ne, left) equal ones come before this one
+        if (gt || (eq && ne < left)) sel[ng + min(ne, left)] = i;
+    }
+    const int32_t n = k + (every > full);
+    for (int32_t i = k + tid; i <= a.top_k; i += 1024) sel[i] = i == k && every > full ? full : -1;
+    if (tid == 0) a.n_sel[row] = n;
+}
+
+}  // namespace wushkv
+
+using namespace wushkv;
+
+int wushkv_validate_cache(const wushkv_cache *c);  // api.hip
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+static int check_bounds(const wushkv_cache *c, const wushkv_bounds *bounds)
+{
+    const int st = wushkv_validate_cache(c);
+    if (st != WUSHKV_OK) return st;
+    if (!bounds || !bounds->codes || !bounds->scales) return WUSHKV_EINVAL;
+    if (!aligned16(bounds->codes) || !aligned16(bounds->scales)) return WUSHKV_EINVAL;
+    return WUSHKV_OK;
+}
+
+extern "C" int wushkv_page_bounds(const wushkv_cache *c, const wushkv_bounds *bounds, const int32_t *since,
+                                  int32_t max_new, wushkv_stream_t stream)
+{
+    const int st = check_bounds(c, bounds);
+    if (st != WUSHKV_OK) return st;
+    if (max_new < 0 || !aligned16(since)) return WUSHKV_EINVAL;
+    if (max_new == 0 || c->n_pages == 0 || c->max_pages_per_seq == 0) return WUSHKV_OK;
+    BoundsArgs a{};
+    a.pages = c->pages;
+    a.page_table = c->page_table;
+    a.seq_len = c->seq_len;
+    a.quant_end = c->quant_end;
+    a.since = since;
+    a.codes = bounds->codes;
+    a.scales = bounds->scales;
+    a.n_kv = c->n_kv_heads;
+    a.s_sink = c->s_sink;
+    a.max_pages = c->max_pages_per_seq;
+    a.n_pages = c->n_pages;
+    a.max_new = max_new < c->max_pages_per_seq ? max_new : c->max_pages_per_seq;
+    const int64_t blocks = ((int64_t)a.max_new * c->n_kv_heads + 3) / 4;
+    if (blocks * c->batch > 0x7FFFFFFF / 4) return WUSHKV_EUNSUPPORTED;
+    a.blocks = (int32_t)blocks;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)(blocks * c->batch));
+    switch (c->head_dim * 10 + storage_bits(c->bits)) {
+        case 1282: launch("page_bounds_kernel", page_bounds_kernel<128, 2>, grid, dim3(256), s, a); break;
+        case 1284: launch("page_bounds_kernel", page_bounds_kernel<128, 4>, grid, dim3(256), s, a); break;
+        case 642: launch("page_bounds_kernel", page_bounds_kernel<64, 2>, grid, dim3(256), s, a); break;
+        case 644: launch("page_bounds_kernel", page_bounds_kernel<64, 4>, grid, dim3(256), s, a); break;
+    }
+    if (hipGetLastError() != hipSuccess) return WUSHKV_ELAUNCH;
+    return WUSHKV_OK;
+}
+
+static int check_select(const wushkv_cache *c, int32_t n_q, int32_t max_seq_len, int32_t top_k)
+{
+    const int st = wushkv_validate_cache(c);
+    if (st != WUSHKV_OK) return st;
+    if (n_q <= 0 || n_q % c->n_kv_heads != 0 || max_seq_len < 0 || top_k < 0 || top_k == INT32_MAX) return WUSHKV_EINVAL;
+    const int32_t G = n_q / c->n_kv_heads;
+    if (G > 8 || (G & (G - 1)) != 0) return WUSHKV_EUNSUPPORTED;
+    if (c->batch > 65535) return WUSHKV_EUNSUPPORTED;
+    return WUSHKV_OK;
+}
+
+extern "C" size_t wushkv_select_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads, int32_t max_seq_len,
+                                                int32_t top_k)
+{
+    if (check_select(c, n_q_heads, max_seq_len, top_k) != WUSHKV_OK) return 0;
+    // the scores (and never nothing, which says that the arguments are bad)
+    return (size_t)c->batch * c->n_kv_heads * c->max_pages_per_seq * sizeof(float) + 16;
+}
+
+template <int D>
+static void launch_select(const SelectArgs &a, int32_t batch, hipStream_t s)
+{
+    constexpr int NT = 256;
+    const dim3 grid((unsigned)a.n_kv, (unsigned)((a.planned + a.run - 1) / a.run), (unsigned)batch);
+    if (grid.y > 0) launch("score_kernel", score_kernel<D, NT>, grid, dim3(NT), s, a);
+    launch("select_kernel", select_kernel, dim3((unsigned)a.n_kv, (unsigned)batch), dim3(1024), s, a);
+}
+
+extern "C" int wushkv_select_pages(const wushkv_cache *c, const wushkv_bounds *bounds, const uint16_t *q,
+                                   int32_t n_q_heads, int32_t max_seq_len, const float *t_k_inv, int32_t top_k,
+                                   int32_t *sel, int32_t *n_sel, float *scores, void *workspace,
+                                   size_t workspace_bytes, wushkv_stream_t stream)
+{
+    int st = check_bounds(c, bounds);
+    if (st != WUSHKV_OK) return st;
+    st = check_select(c, n_q_heads, max_seq_len, top_k);
+    if (st != WUSHKV_OK) return st;
+    if (!q || !t_k_inv || !sel || !n_sel || !workspace) return WUSHKV_EINVAL;
+    if (!aligned16(q) || !aligned16(t_k_inv) || !aligned16(sel) || !aligned16(n_sel) || !aligned16(scores) ||
+        !aligned16(workspace))
+        return WUSHKV_EINVAL;
+    if (workspace_bytes < wushkv_select_workspace_bytes(c, n_q_heads, max_seq_len, top_k)) return WUSHKV_EWORKSPACE;
+    SelectArgs a{};
+    a.codes = bounds->codes;
+    a.scales = bounds->scales;
+    a.page_table = c->page_table;
+    a.seq_len = c->seq_len;
+    a.quant_end = c->quant_end;
+    a.q = q;
+    a.tinv = t_k_inv;
+    a.sel = sel;
+    a.n_sel = n_sel;
+    a.scores = scores != nullptr ? scores : reinterpret_cast<float *>(workspace);
+    a.n_kv = c->n_kv_heads;
+    a.G = n_q_heads / c->n_kv_heads;
+    a.s_sink = c->s_sink;
+    a.max_pages = c->max_pages_per_seq;
+    a.n_pages = c->n_pages;
+    const int64_t span = (int64_t)max_seq_len - c->s_sink;
+    const int64_t pages = span > 0 ? (span + kPage - 1) / kPage : 0;
+    a.planned = (int32_t)(pages < c->max_pages_per_seq ? pages : c->max_pages_per_seq);
+    if (c->page_table == nullptr) a.planned = 0;
+    a.run = 128;
+    while ((a.planned + a.run - 1) / a.run > 65535) a.run *= 2;
+    a.top_k = top_k;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (c->head_dim == 128) launch_select<128>(a, c->batch, s);
+    else launch_select<64>(a, c->batch, s);
+    if (hipGetLastError() != hipSuccess) return WUSHKV_ELAUNCH;
+    return WUSHKV_OK;
+}
