@@ -123,6 +123,7 @@ struct DecodeArgs {
     const int32_t *n_sel;  // [batch][n_kv]
     int32_t max_sel;
     float mid;             // the middle of the key codes, (2^bits - 1) / 2
+    float *out;            // ONE: [batch][n_q][D]
 };
 
 // Tokens of sequence b's chunk: n_tok[b] (or max_tok), at most max_tok and
@@ -791,12 +792,17 @@ __device__ __forceinline__ PageRun plan_runs(const DecodeArgs &a, const RunCount
 // token groups) and every wave writes its own partials.
 // LIST: a run is a run of the (sequence, kv head)'s list of logical pages; a
 // lane then keeps its entry's logical page beside the physical one.
-template <int D, int BITS, int G, bool FORM, bool SHARE, bool LIST = false>
+// ONE (with LIST and FORM): one workgroup takes a row's whole list and windows.
+// Each wave goes over its window tiles while its first pages are in flight,
+// carries their sums on as the start of its pages' softmax, and the merge of the
+// four waves is the output: no partials, no second launch.
+template <int D, int BITS, int G, bool FORM, bool SHARE, bool LIST = false, bool ONE = false>
 __global__ void __launch_bounds__(256, ((D == 128 && (BITS == 4 || (G == 8 && !SHARE))) || (D == 64 && BITS == 4 && G == 8)) ? 2 : 3)
 decode_main_kernel(DecodeArgs a)
 {
     static_assert(!(FORM && SHARE), "shared work items take q~ from decode_qt_kernel");
     static_assert(!(LIST && SHARE), "a list belongs to one query row");
+    static_assert(!ONE || (LIST && FORM), "whole rows are lists with their q~ formed here");
     using L = Layout<D, BITS>;
     using M = MainLds<D, BITS, G>;
     constexpr bool kEarly = FORM && M::kEarly;
@@ -835,7 +841,7 @@ decode_main_kernel(DecodeArgs a)
     // What needs no counter is requested first: the T^{-1} entries and queries
     // of q~, and the page-table entries of this wave's run (a run's share
     // beyond the sequence's pages is not used)
-    const bool page_wg = split < a.n_page_splits;
+    const bool page_wg = ONE || split < a.n_page_splits;
     const int upw = a.units_per_wave;
     int w0 = page_wg ? (SHARE ? split : split * 4 + wave) * upw : 0;
     // (the counters of plan_runs before those: loads complete in order)
@@ -902,27 +908,277 @@ decode_main_kernel(DecodeArgs a)
     uint8_t *qrows = lds + M::kRowsAt;
     const int64_t row0 = ((int64_t)bz * a.n_kv + h) * G;  // first (virtual) query head
 
-    if (page_wg) {
-        // ================================================ quantised pages
-        auto phys_of = [&](int u) -> int32_t { return __builtin_amdgcn_readlane(tbl, u - w0); };
-        // Every page of the run issues exactly kDma loads; an entry outside
-        // the pool loads physical page 0 instead (its data is never used),
-        // which keeps the count of outstanding loads a closed form.
-        auto issue = [&](int u, int s) {
-            int32_t phys = phys_of(u);
-            if (phys < 0 || phys >= a.n_pages) phys = 0;
-            const uint8_t *src = a.pages + ((int64_t)phys * a.n_kv + h) * L::kPageBytes + 16 * lane;
-            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(stage + s * kSlot));
+    auto phys_of = [&](int u) -> int32_t { return __builtin_amdgcn_readlane(tbl, u - w0); };
+    // Every page of the run issues exactly kDma loads; an entry outside
+    // the pool loads physical page 0 instead (its data is never used),
+    // which keeps the count of outstanding loads a closed form.
+    auto issue = [&](int u, int s) {
+        int32_t phys = phys_of(u);
+        if (phys < 0 || phys >= a.n_pages) phys = 0;
+        const uint8_t *src = a.pages + ((int64_t)phys * a.n_kv + h) * L::kPageBytes + 16 * lane;
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(stage + s * kSlot));
 #pragma unroll
-            for (int i = 0; i < kDma; ++i) {
-                if (i + 1 < kDma || 1024 * i + 16 * lane < L::kPageBytes)
-                    dma16(src + 1024 * i, dst + 1024 * i);
+        for (int i = 0; i < kDma; ++i) {
+            if (i + 1 < kDma || 1024 * i + 16 * lane < L::kPageBytes)
+                dma16(src + 1024 * i, dst + 1024 * i);
+        }
+    };
+    const bool run = a.n_pages > 0 && w0 < w1;
+    // ONE: q~ first, then the windows, then the pages
+    f32x4 win_acc[ONE ? kNT : 1];
+    float win_m[2], win_l[2];
+    if constexpr (ONE) {
+        static_assert(kEarly || Q::kBytes <= M::kStageBytes, "the rows lie clear of the weight buffers");
+        stage_queries(qin, qrows, tid);
+        if (kEarly) {  // (as below)
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+            if (run) {
+                issue(w0, 0);
+                if (w0 + 1 < w1) issue(w0 + 1, 1);
+            }
+        }
+        form_qt<D, G>(a, qin, qrows, tid);
+    }
+
+    if (ONE || !page_wg) {
+        // ================================================ window slots
+        // Workgroup n_page_splits + u owns window unit u (slots 64 u ..
+        // 64 u + 63), wave w its 16 slots 64 u + 16 w .. + 15 (SHARE: the
+        // workgroup owns win_units consecutive units and every wave all their
+        // 16-slot tiles, for its own rows, with an online softmax across
+        // them).  All of a tile's loads are issued together.
+        const int32_t ring = a.win_slots - a.s_sink;
+        // the ring holds positions [q_hi, S); the oldest sits at ring index a0
+        const int32_t a0 = S > q_hi ? (q_hi - a.s_sink) % ring : 0;
+        const int32_t ring_live = S > q_hi ? S - q_hi : 0;
+        const int64_t head_win = ((int64_t)b * a.n_kv + h) * a.win_slots;
+        const int32_t unit0 = ONE ? 0 : (split - a.n_page_splits) * kPage * a.win_units;
+        // fused step: the workgroup whose unit holds the new token's slot
+        // writes the token and keeps it in LDS, at the end of wave 3's page
+        // stage (its merge rows, written last, sit at the start)
+        int32_t new_slot = -1;
+        uint16_t *tok = reinterpret_cast<uint16_t *>(lds + 3 * M::kWave + M::kStageBytes - 4 * D);
+        static_assert(G * D * 4 + 8 * D <= M::kStageBytes, "the new token fits the page stage");
+        if (a.n_new != nullptr && nn > 0) {
+            const int32_t slot = s_old < a.s_sink ? s_old : ring_slot(s_old, a.s_sink, ring);
+            if (slot >= unit0 && slot < unit0 + kPage * a.win_units) {
+                new_slot = slot;
+                step_token<D>(a, b, h, slot, tok, tid);
+            }
+        }
+
+        const float *qtl;
+        if constexpr (FORM) {
+            if constexpr (!ONE) {
+                stage_queries(qin, qrows, tid);
+                form_qt<D, G>(a, qin, qrows, tid);
+            }
+            qtl = reinterpret_cast<const float *>(qrows);
+        } else {
+            qtl = a.qt + row0 * D;
+        }
+        // A operands: row m = 2 g + part (hi, lo) of q~, chunk c.  From LDS
+        // they are formed at once; from memory only after the slot loads are
+        // issued, so that the latencies overlap.
+        // LIST: a third part of q~ and of the weights, in operands of their own
+        // that add onto the hi rows (two parts leave 2^-18 of the largest, and
+        // with few pages the windows are most of the attention)
+        bf16x8 qa[kC], qa3[LIST ? kC : 1];
+        auto form_qa = [&]() {
+            const int g = n >> 1, part = n & 1;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                uint32_t u[4] = {0u, 0u, 0u, 0u}, u3[4] = {0u, 0u, 0u, 0u};
+                if (g < G) {
+                    const float *src = qtl + g * D + 32 * c + 8 * j;
+                    const f32x4 x0 = *reinterpret_cast<const f32x4 *>(src);
+                    const f32x4 x1 = *reinterpret_cast<const f32x4 *>(src + 4);
+                    const float x[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+#pragma unroll
+                    for (int pp = 0; pp < 4; ++pp) {
+                        const uint32_t hi = pack_bf16_rne(x[2 * pp], x[2 * pp + 1]);
+                        const uint32_t lo = pack_bf16_rne(x[2 * pp] - bf16_bits_to_f32(hi & 0xFFFFu),
+                                                          x[2 * pp + 1] - bf16_bits_to_f32(hi >> 16));
+                        u[pp] = part ? lo : hi;
+                        if constexpr (LIST) {
+                            const float e0 = x[2 * pp] - bf16_bits_to_f32(hi & 0xFFFFu) - bf16_bits_to_f32(lo & 0xFFFFu);
+                            const float e1 = x[2 * pp + 1] - bf16_bits_to_f32(hi >> 16) - bf16_bits_to_f32(lo >> 16);
+                            u3[pp] = part ? 0u : pack_bf16_rne(e0, e1);
+                        }
+                    }
+                }
+                qa[c] = __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]});
+                if constexpr (LIST) qa3[c] = __builtin_bit_cast(bf16x8, u32x4{u3[0], u3[1], u3[2], u3[3]});
             }
         };
-        const bool run = a.n_pages > 0 && w0 < w1;
+        if constexpr (FORM) form_qa();
+        if constexpr (FORM && !kEarly && !ONE) __syncthreads();  // the rows may now be overwritten
+        if (lane < 16) reinterpret_cast<uint32_t *>(tbuf + M::kTRows * kTP)[lane] = 0u;
+
+        f32x4 acc[kNT];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) acc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float m_run[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
+        bool formed = FORM;
+        // SHARE: every wave all 16-slot tiles of the workgroup's units, with
+        // an online softmax across them
+        // (otherwise wave w takes tile w of each of the workgroup's units)
+        // (the query-forming variant runs only plans of one unit per window
+        // workgroup: its loop is a single tile, kept compile-time so that it
+        // costs no registers)
+        const int kSub = SHARE ? 4 * a.win_units : (FORM && !ONE ? 1 : a.win_units);
+        for (int st = 0; st < (rows_live ? kSub : 0); ++st) {
+            const int32_t slot0 = unit0 + 16 * (SHARE ? st : wave + 4 * st);
+            // this tile's live slots, one bit per slot (lanes 0..15)
+            bool mine;
+            {
+                const int32_t sl = slot0 + n;
+                if (sl < a.s_sink) mine = sl < S;
+                else mine = ((sl - a.s_sink - a0 + ring) % ring) < ring_live;
+            }
+            const uint32_t vmask = (uint32_t)(__ballot(mine) & 0xFFFFu);
+            if (vmask == 0) continue;
+            // key slots (token slot0 + n, channels 32 c + 8 j ..) and value
+            // slots (channel 16 nt + n, tokens slot0 + 4 j .. + 3)
+            const uint16_t *krow = a.win_k + (head_win + slot0 + n) * D + 8 * j;
+            u32x4 kx[kC];
+#pragma unroll
+            for (int c = 0; c < kC; ++c) kx[c] = *reinterpret_cast<const u32x4 *>(krow + 32 * c);
+            const uint16_t *vrow = a.win_v + head_win * D + slot0 + 4 * j;
+            u32x2 vx[kNT];
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+                vx[nt] = *reinterpret_cast<const u32x2 *>(vrow + (int64_t)(16 * nt + n) * a.win_slots);
+            if (new_slot >= slot0 && new_slot < slot0 + 16) {
+                // the new token's slot: its key row (lanes n = t) and its
+                // values (element t % 4 of lanes j = t / 4) from LDS
+                const int t = new_slot - slot0;
+                if (n == t) {
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) kx[c] = *reinterpret_cast<const u32x4 *>(tok + 32 * c + 8 * j);
+                }
+                if (j == (t >> 2)) {
+                    const int e = t & 3;
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        const uint32_t v = tok[D + 16 * nt + n];
+                        const uint32_t w = vx[nt][e >> 1];
+                        vx[nt][e >> 1] = (e & 1) ? ((w & 0xFFFFu) | (v << 16)) : ((w & 0xFFFF0000u) | v);
+                    }
+                }
+            }
+            if (!formed) {
+                form_qa();
+                formed = true;
+            }
+
+            // scores: lane (j, n) gets rows 4 j + r = (head 2 j + r / 2,
+            // part r % 2) of token slot0 + n
+            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < kC; ++c) sc = mfma16(qa[c], __builtin_bit_cast(bf16x8, kx[c]), sc);
+            if constexpr (LIST) {
+#pragma unroll
+                for (int c = 0; c < kC; ++c) sc = mfma16(qa3[c], __builtin_bit_cast(bf16x8, kx[c]), sc);
+            }
+            const bool ok = (vmask >> n) & 1u;
+            // causal visibility of this slot's position to the query rows
+            // 2 j and 2 j + 1: a chunk token at position p sees [0, p] (the
+            // quantised pages all lie before the chunk, so only the windows
+            // need this)
+            bool vis[2] = {ok, ok};  // decode: the query sees every live slot
+            if (a.max_tok > 1 || a.n_tok != nullptr) {
+                const int32_t sl = slot0 + n;
+                const int32_t pos = sl < a.s_sink ? sl : q_hi + ((sl - a.s_sink - a0 + ring) % ring);
+                const int32_t nb = chunk_tokens(a.n_tok, a.max_tok, b, S);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int32_t t = tg * a.tpg + (2 * j + e) / a.g_real;  // chunk token of the row
+                    vis[e] = ok && t < nb && pos <= S - nb + t;
+                }
+            }
+            float lg[2];
+            lg[0] = vis[0] ? sc[0] + sc[1] : -INFINITY;
+            lg[1] = vis[1] ? sc[2] + sc[3] : -INFINITY;
+            float pr[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                // online softmax over the tiles: the running sums are scaled
+                // to the new maximum (a first tile scales zeros)
+                const float m_new = fmaxf(m_run[e], row_max16(lg[e]));
+                const float f_old = m_run[e] == -INFINITY ? 0.0f : fexp2(m_run[e] - m_new);
+                pr[e] = m_new == -INFINITY ? 0.0f : fexp2(lg[e] - m_new);
+                lsum[e] = fmaf(lsum[e], f_old, pr[e]);
+                m_run[e] = m_new;
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt) {
+                    acc[nt][2 * e] *= f_old;
+                    acc[nt][2 * e + 1] *= f_old;
+                }
+                const int g = 2 * j + e;
+                if (g < G) {
+                    const uint32_t hl = pack_bf16_rne(pr[e], 0.0f) & 0xFFFFu;
+                    const uint32_t ll = pack_bf16_rne(pr[e] - bf16_bits_to_f32(hl), 0.0f) & 0xFFFFu;
+                    lds_write2(lds_addr(tbuf + g * kTP + 2 * n), hl);
+                    lds_write2(lds_addr(tbuf + (G + g) * kTP + 2 * n), ll);
+                    if constexpr (LIST)  // (the upper half of the head's hi row)
+                        lds_write2(lds_addr(tbuf + g * kTP + 64 + 2 * n),
+                                   pack_bf16_rne(pr[e] - bf16_bits_to_f32(hl) - bf16_bits_to_f32(ll), 0.0f) & 0xFFFFu);
+                }
+            }
+            // A operand of the 16x16x16 product: row m = 2 g + part, tokens
+            // 4 j .. 4 j + 3
+            const uint32_t pa_addr = n < 2 * G ? lds_addr(tbuf + ((n & 1) * G + (n >> 1)) * kTP + 8 * j) : zero_row;
+            const u32x2 pa = lds_read8(pa_addr);
+            // dead slots' values are zeroed, whatever bits they hold
+            const uint32_t bits4 = (vmask >> (4 * j)) & 0xFu;
+            const uint32_t msk0 = ((bits4 & 1u) ? 0x0000FFFFu : 0u) | ((bits4 & 2u) ? 0xFFFF0000u : 0u);
+            const uint32_t msk1 = ((bits4 & 4u) ? 0x0000FFFFu : 0u) | ((bits4 & 8u) ? 0xFFFF0000u : 0u);
+            typedef __attribute__((ext_vector_type(4))) short s16x4;
+            const s16x4 A = __builtin_bit_cast(s16x4, pa);
+            s16x4 A3 = A;
+            if constexpr (LIST) {
+                const bool third = n < 2 * G && (n & 1) == 0;
+                A3 = __builtin_bit_cast(s16x4, lds_read8(third ? pa_addr + 64u : zero_row));
+            }
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+                const u32x2 y = {vx[nt][0] & msk0, vx[nt][1] & msk1};
+                acc[nt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(A, __builtin_bit_cast(s16x4, y), acc[nt], 0, 0, 0);
+                if constexpr (LIST)
+                    acc[nt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(A3, __builtin_bit_cast(s16x4, y), acc[nt], 0, 0, 0);
+            }
+        }
+        if constexpr (ONE) {
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) win_acc[nt] = acc[nt];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                win_m[e] = m_run[e];
+                win_l[e] = lsum[e];
+            }
+        } else {
+            // result per head g = 2 j + e: rows 4 j + 2 e (hi) and + 1 (lo)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int g = 2 * j + e;
+                const float lt = row_sum16(lsum[e]);
+                if (g < G) {
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) sC[g][16 * nt + n] = acc[nt][2 * e] + acc[nt][2 * e + 1];
+                    if (n == 0) {
+                        sM[wave][g] = m_run[e];
+                        sL[wave][g] = lt;
+                    }
+                }
+            }
+        }
+    }
+    if (page_wg) {
+        // ================================================ quantised pages
         const uint8_t *qlimb;
         const uint32_t *qaux;
-        if constexpr (FORM) {
+        if constexpr (FORM && !ONE) {
             // When the rows have LDS of their own, the first two pages of the
             // run go in flight while q~ is formed.  Every load made so far
             // completes first, so that no later wait of the rows' arithmetic
@@ -938,6 +1194,8 @@ decode_main_kernel(DecodeArgs a)
                 }
             }
             form_qt<D, G>(a, qin, qrows, tid);
+        }
+        if constexpr (FORM) {
             form_limbs<D, BITS, G>(qrows, tid);
             qlimb = qrows;
             qaux = reinterpret_cast<const uint32_t *>(qrows + Q::kAux);
@@ -1038,6 +1296,49 @@ decode_main_kernel(DecodeArgs a)
         WidenNormal<BITS> wide;
         if constexpr (LIST) wide.init();
 
+        if constexpr (ONE) {
+            // the wave's window sums, relative to the reference, from their rows
+            // to those of the pages' sums (through the weight buffer, 64 channels
+            // at a time); one lane of a row carries l
+            float *tb = reinterpret_cast<float *>(tbuf);
+            const float up = ldexpf(1.0f, (int)lift);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int g = 2 * j + e;
+                const float lt = row_sum16(win_l[e]);
+                if (g < G && n == 0) {
+                    sM[wave][g] = win_m[e];
+                    sL[wave][g] = lt * up;
+                }
+            }
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int g = 2 * j + e;
+                        if (g < G) tb[64 * g + 16 * i + n] = win_acc[4 * half + i][2 * e] + win_acc[4 * half + i][2 * e + 1];
+                    }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int hg = 0; hg < kHG; ++hg)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int hs = G > 4 ? 2 * j + hg : j;
+                        if (hs < G) acc[4 * half + i][G > 4 ? 2 * hg : 0] = tb[64 * hs + 16 * i + n] * (up / kOutScale);
+                    }
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int hg = 0; hg < kHG; ++hg) {
+                const int hs = G > 4 ? 2 * j + hg : j;
+                if (hs < G) {
+                    m_run[hg] = sM[wave][hs];
+                    if (n == 0) lc[hg] = sL[wave][hs];
+                }
+            }
+        }
         // P V A operand rows: row m is part m % kRowsPerHead (0: fp16 hi
         // of the weight, 1: the fp16 rest, others zero) of head
         // m / kRowsPerHead; weight rows sit at 2 g + part in the buffer
@@ -1275,227 +1576,6 @@ decode_main_kernel(DecodeArgs a)
                 }
             }
         }
-    } else {
-        // ================================================ window slots
-        // Workgroup n_page_splits + u owns window unit u (slots 64 u ..
-        // 64 u + 63), wave w its 16 slots 64 u + 16 w .. + 15 (SHARE: the
-        // workgroup owns win_units consecutive units and every wave all their
-        // 16-slot tiles, for its own rows, with an online softmax across
-        // them).  All of a tile's loads are issued together.
-        const int32_t ring = a.win_slots - a.s_sink;
-        // the ring holds positions [q_hi, S); the oldest sits at ring index a0
-        const int32_t a0 = S > q_hi ? (q_hi - a.s_sink) % ring : 0;
-        const int32_t ring_live = S > q_hi ? S - q_hi : 0;
-        const int64_t head_win = ((int64_t)b * a.n_kv + h) * a.win_slots;
-        const int32_t unit0 = (split - a.n_page_splits) * kPage * a.win_units;
-        // fused step: the workgroup whose unit holds the new token's slot
-        // writes the token and keeps it in LDS, at the end of wave 3's page
-        // stage (its merge rows, written last, sit at the start)
-        int32_t new_slot = -1;
-        uint16_t *tok = reinterpret_cast<uint16_t *>(lds + 3 * M::kWave + M::kStageBytes - 4 * D);
-        static_assert(G * D * 4 + 8 * D <= M::kStageBytes, "the new token fits the page stage");
-        if (a.n_new != nullptr && nn > 0) {
-            const int32_t slot = s_old < a.s_sink ? s_old : ring_slot(s_old, a.s_sink, ring);
-            if (slot >= unit0 && slot < unit0 + kPage * a.win_units) {
-                new_slot = slot;
-                step_token<D>(a, b, h, slot, tok, tid);
-            }
-        }
-
-        const float *qtl;
-        if constexpr (FORM) {
-            stage_queries(qin, qrows, tid);
-            form_qt<D, G>(a, qin, qrows, tid);
-            qtl = reinterpret_cast<const float *>(qrows);
-        } else {
-            qtl = a.qt + row0 * D;
-        }
-        // A operands: row m = 2 g + part (hi, lo) of q~, chunk c.  From LDS
-        // they are formed at once; from memory only after the slot loads are
-        // issued, so that the latencies overlap.
-        // LIST: a third part of q~ and of the weights, in operands of their own
-        // that add onto the hi rows (two parts leave 2^-18 of the largest, and
-        // with few pages the windows are most of the attention)
-        bf16x8 qa[kC], qa3[LIST ? kC : 1];
-        auto form_qa = [&]() {
-            const int g = n >> 1, part = n & 1;
-#pragma unroll
-            for (int c = 0; c < kC; ++c) {
-                uint32_t u[4] = {0u, 0u, 0u, 0u}, u3[4] = {0u, 0u, 0u, 0u};
-                if (g < G) {
-                    const float *src = qtl + g * D + 32 * c + 8 * j;
-                    const f32x4 x0 = *reinterpret_cast<const f32x4 *>(src);
-                    const f32x4 x1 = *reinterpret_cast<const f32x4 *>(src + 4);
-                    const float x[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
-#pragma unroll
-                    for (int pp = 0; pp < 4; ++pp) {
-                        const uint32_t hi = pack_bf16_rne(x[2 * pp], x[2 * pp + 1]);
-                        const uint32_t lo = pack_bf16_rne(x[2 * pp] - bf16_bits_to_f32(hi & 0xFFFFu),
-                                                          x[2 * pp + 1] - bf16_bits_to_f32(hi >> 16));
-                        u[pp] = part ? lo : hi;
-                        if constexpr (LIST) {
-                            const float e0 = x[2 * pp] - bf16_bits_to_f32(hi & 0xFFFFu) - bf16_bits_to_f32(lo & 0xFFFFu);
-                            const float e1 = x[2 * pp + 1] - bf16_bits_to_f32(hi >> 16) - bf16_bits_to_f32(lo >> 16);
-                            u3[pp] = part ? 0u : pack_bf16_rne(e0, e1);
-                        }
-                    }
-                }
-                qa[c] = __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]});
-                if constexpr (LIST) qa3[c] = __builtin_bit_cast(bf16x8, u32x4{u3[0], u3[1], u3[2], u3[3]});
-            }
-        };
-        if constexpr (FORM) form_qa();
-        if constexpr (FORM && !kEarly) __syncthreads();  // the rows may now be overwritten
-        if (lane < 16) reinterpret_cast<uint32_t *>(tbuf + M::kTRows * kTP)[lane] = 0u;
-
-        f32x4 acc[kNT];
-#pragma unroll
-        for (int nt = 0; nt < kNT; ++nt) acc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m_run[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
-        bool formed = FORM;
-        // SHARE: every wave all 16-slot tiles of the workgroup's units, with
-        // an online softmax across them
-        // (otherwise wave w takes tile w of each of the workgroup's units)
-        // (the query-forming variant runs only plans of one unit per window
-        // workgroup: its loop is a single tile, kept compile-time so that it
-        // costs no registers)
-        const int kSub = SHARE ? 4 * a.win_units : (FORM ? 1 : a.win_units);
-        for (int st = 0; st < (rows_live ? kSub : 0); ++st) {
-            const int32_t slot0 = unit0 + 16 * (SHARE ? st : wave + 4 * st);
-            // this tile's live slots, one bit per slot (lanes 0..15)
-            bool mine;
-            {
-                const int32_t sl = slot0 + n;
-                if (sl < a.s_sink) mine = sl < S;
-                else mine = ((sl - a.s_sink - a0 + ring) % ring) < ring_live;
-            }
-            const uint32_t vmask = (uint32_t)(__ballot(mine) & 0xFFFFu);
-            if (vmask == 0) continue;
-            // key slots (token slot0 + n, channels 32 c + 8 j ..) and value
-            // slots (channel 16 nt + n, tokens slot0 + 4 j .. + 3)
-            const uint16_t *krow = a.win_k + (head_win + slot0 + n) * D + 8 * j;
-            u32x4 kx[kC];
-#pragma unroll
-            for (int c = 0; c < kC; ++c) kx[c] = *reinterpret_cast<const u32x4 *>(krow + 32 * c);
-            const uint16_t *vrow = a.win_v + head_win * D + slot0 + 4 * j;
-            u32x2 vx[kNT];
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt)
-                vx[nt] = *reinterpret_cast<const u32x2 *>(vrow + (int64_t)(16 * nt + n) * a.win_slots);
-            if (new_slot >= slot0 && new_slot < slot0 + 16) {
-                // the new token's slot: its key row (lanes n = t) and its
-                // values (element t % 4 of lanes j = t / 4) from LDS
-                const int t = new_slot - slot0;
-                if (n == t) {
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) kx[c] = *reinterpret_cast<const u32x4 *>(tok + 32 * c + 8 * j);
-                }
-                if (j == (t >> 2)) {
-                    const int e = t & 3;
-#pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt) {
-                        const uint32_t v = tok[D + 16 * nt + n];
-                        const uint32_t w = vx[nt][e >> 1];
-                        vx[nt][e >> 1] = (e & 1) ? ((w & 0xFFFFu) | (v << 16)) : ((w & 0xFFFF0000u) | v);
-                    }
-                }
-            }
-            if (!formed) {
-                form_qa();
-                formed = true;
-            }
-
-            // scores: lane (j, n) gets rows 4 j + r = (head 2 j + r / 2,
-            // part r % 2) of token slot0 + n
-            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < kC; ++c) sc = mfma16(qa[c], __builtin_bit_cast(bf16x8, kx[c]), sc);
-            if constexpr (LIST) {
-#pragma unroll
-                for (int c = 0; c < kC; ++c) sc = mfma16(qa3[c], __builtin_bit_cast(bf16x8, kx[c]), sc);
-            }
-            const bool ok = (vmask >> n) & 1u;
-            // causal visibility of this slot's position to the query rows
-            // 2 j and 2 j + 1: a chunk token at position p sees [0, p] (the
-            // quantised pages all lie before the chunk, so only the windows
-            // need this)
-            bool vis[2] = {ok, ok};  // decode: the query sees every live slot
-            if (a.max_tok > 1 || a.n_tok != nullptr) {
-                const int32_t sl = slot0 + n;
-                const int32_t pos = sl < a.s_sink ? sl : q_hi + ((sl - a.s_sink - a0 + ring) % ring);
-                const int32_t nb = chunk_tokens(a.n_tok, a.max_tok, b, S);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int32_t t = tg * a.tpg + (2 * j + e) / a.g_real;  // chunk token of the row
-                    vis[e] = ok && t < nb && pos <= S - nb + t;
-                }
-            }
-            float lg[2];
-            lg[0] = vis[0] ? sc[0] + sc[1] : -INFINITY;
-            lg[1] = vis[1] ? sc[2] + sc[3] : -INFINITY;
-            float pr[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                // online softmax over the tiles: the running sums are scaled
-                // to the new maximum (a first tile scales zeros)
-                const float m_new = fmaxf(m_run[e], row_max16(lg[e]));
-                const float f_old = m_run[e] == -INFINITY ? 0.0f : fexp2(m_run[e] - m_new);
-                pr[e] = m_new == -INFINITY ? 0.0f : fexp2(lg[e] - m_new);
-                lsum[e] = fmaf(lsum[e], f_old, pr[e]);
-                m_run[e] = m_new;
-#pragma unroll
-                for (int nt = 0; nt < kNT; ++nt) {
-                    acc[nt][2 * e] *= f_old;
-                    acc[nt][2 * e + 1] *= f_old;
-                }
-                const int g = 2 * j + e;
-                if (g < G) {
-                    const uint32_t hl = pack_bf16_rne(pr[e], 0.0f) & 0xFFFFu;
-                    const uint32_t ll = pack_bf16_rne(pr[e] - bf16_bits_to_f32(hl), 0.0f) & 0xFFFFu;
-                    lds_write2(lds_addr(tbuf + g * kTP + 2 * n), hl);
-                    lds_write2(lds_addr(tbuf + (G + g) * kTP + 2 * n), ll);
-                    if constexpr (LIST)  // (the upper half of the head's hi row)
-                        lds_write2(lds_addr(tbuf + g * kTP + 64 + 2 * n),
-                                   pack_bf16_rne(pr[e] - bf16_bits_to_f32(hl) - bf16_bits_to_f32(ll), 0.0f) & 0xFFFFu);
-                }
-            }
-            // A operand of the 16x16x16 product: row m = 2 g + part, tokens
-            // 4 j .. 4 j + 3
-            const uint32_t pa_addr = n < 2 * G ? lds_addr(tbuf + ((n & 1) * G + (n >> 1)) * kTP + 8 * j) : zero_row;
-            const u32x2 pa = lds_read8(pa_addr);
-            // dead slots' values are zeroed, whatever bits they hold
-            const uint32_t bits4 = (vmask >> (4 * j)) & 0xFu;
-            const uint32_t msk0 = ((bits4 & 1u) ? 0x0000FFFFu : 0u) | ((bits4 & 2u) ? 0xFFFF0000u : 0u);
-            const uint32_t msk1 = ((bits4 & 4u) ? 0x0000FFFFu : 0u) | ((bits4 & 8u) ? 0xFFFF0000u : 0u);
-            typedef __attribute__((ext_vector_type(4))) short s16x4;
-            const s16x4 A = __builtin_bit_cast(s16x4, pa);
-            s16x4 A3 = A;
-            if constexpr (LIST) {
-                const bool third = n < 2 * G && (n & 1) == 0;
-                A3 = __builtin_bit_cast(s16x4, lds_read8(third ? pa_addr + 64u : zero_row));
-            }
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) {
-                const u32x2 y = {vx[nt][0] & msk0, vx[nt][1] & msk1};
-                acc[nt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(A, __builtin_bit_cast(s16x4, y), acc[nt], 0, 0, 0);
-                if constexpr (LIST)
-                    acc[nt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(A3, __builtin_bit_cast(s16x4, y), acc[nt], 0, 0, 0);
-            }
-        }
-        // result per head g = 2 j + e: rows 4 j + 2 e (hi) and + 1 (lo)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int g = 2 * j + e;
-            const float lt = row_sum16(lsum[e]);
-            if (g < G) {
-#pragma unroll
-                for (int nt = 0; nt < kNT; ++nt) sC[g][16 * nt + n] = acc[nt][2 * e] + acc[nt][2 * e + 1];
-                if (n == 0) {
-                    sM[wave][g] = m_run[e];
-                    sL[wave][g] = lt;
-                }
-            }
-        }
     }
     __syncthreads();
 
@@ -1534,6 +1614,10 @@ decode_main_kernel(DecodeArgs a)
                 o += f * reinterpret_cast<const float(*)[D]>(lds + w * M::kWave)[gg][ch];
                 l += f * sL[w][gg];
             }
+        }
+        if constexpr (ONE) {
+            a.out[((int64_t)b * a.n_kv * G + h * G + gg) * D + ch] = l > 0.0f ? o / l : 0.0f;
+            continue;
         }
         part[gg * (D + 2) + ch] = o;
         if (ch == 0) {
@@ -2485,7 +2569,9 @@ static void launch_main(bool form, bool share, dim3 grid, unsigned rows_z, hipSt
 {
     const bool list = a.n_sel != nullptr;
     if (form) {
-        if (list)
+        if (a.out != nullptr)
+            launch("sparse_row_kernel", decode_main_kernel<D, BITS, G, true, false, true, true>, grid, dim3(256), s, a);
+        else if (list)
             launch("sparse_main_kernel", decode_main_kernel<D, BITS, G, true, false, true>, grid, dim3(256), s, a);
         else
             launch("decode_main_kernel", decode_main_kernel<D, BITS, G, true, false>, grid, dim3(256), s, a);
@@ -2536,6 +2622,21 @@ static int check_chunk(const wushkv_cache *c, int32_t max_tok)
     return WUSHKV_OK;
 }
 
+// Lists: whether one workgroup takes a row's whole list and its windows.  With
+// a row for every compute unit the rows fill the device by themselves, and the
+// launch of q~, the partials and their merge fall away (d = 128, four heads,
+// 2-bit, 512 rows of 5, 33 and 65 pages: 19.8, 34.9 and 51.0 us a call instead of
+// 33.5, 47.1 and 60.9; eight heads, 4-bit, 256 rows of 129: 76 and 83).  With
+// fewer rows compute units would stand idle (128 rows of 65: 29 us, split 22; 64
+// rows of 129, 44 and 20).  A list of at most 8 pages of d = 64 is a chain of two
+// pages a wave, shorter than the second launch (9.3 us, split 11.2).  A wave's
+// pages are numbered by its lanes.
+static bool whole_rows(const wushkv_cache *c, int32_t max_sel)
+{
+    if (max_sel > 4 * kMaxRunPages) return false;
+    return (int64_t)c->batch * c->n_kv_heads >= device_cus() || (c->head_dim == 64 && max_sel <= 8);
+}
+
 static size_t plan_bytes(const DecodePlan &p)
 {
     return p.qt_bytes + p.limb_bytes + p.aux_bytes + p.part_bytes;
@@ -2578,6 +2679,7 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
     if (!(sm_scale > 0.0f) || sm_scale == INFINITY) return WUSHKV_EINVAL;
     const RowShape rs = row_shape(c, n_q_heads, max_tok);
     DecodePlan p;
+    const bool whole = list != nullptr && whole_rows(c, list->max_sel);
     if (!make_plan(c, rs, list != nullptr ? list->max_sel : pages_of(c, max_seq_len), p)) return WUSHKV_EUNSUPPORTED;
     if (workspace_bytes < plan_bytes(p)) return WUSHKV_EWORKSPACE;
 
@@ -2632,6 +2734,12 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
         a.max_sel = list->max_sel;
         a.mid = 0.5f * ((1 << c->bits) - 1);
     }
+    if (whole) {
+        a.out = out;
+        a.units_per_wave = list->max_sel > 4 ? (list->max_sel + 3) / 4 : 1;
+        a.n_page_splits = a.n_splits = p.n_page_splits = p.n_splits = 1;
+        a.win_units = c->win_slots / kPage;
+    }
 
     const unsigned rows_z = (unsigned)(c->batch * rs.n_groups);
     // several token groups (a chunk of more tokens than one group holds):
@@ -2645,8 +2753,8 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
     // that read once per workgroup, so a small kernel forms q~ first; so do
     // grids of shared work items.
     const int64_t wgs = (int64_t)p.n_splits * c->n_kv_heads * grid_z;
-    const bool form = !rs.share && p.win_units == 1 &&
-                      wgs * 4 <= resident_waves(c->head_dim, storage_bits(c->bits), G, false);
+    const bool form = whole || (!rs.share && p.win_units == 1 &&
+                                wgs * 4 <= resident_waves(c->head_dim, storage_bits(c->bits), G, false));
     // such a grid also deals its page runs out by the lengths it finds (one
     // lane per sequence), noted where the query rows' aux words would be; a
     // chunk of one token as a decode, whose bits it keeps
@@ -2679,6 +2787,7 @@ static int attend(const wushkv_cache *c, const uint16_t *q, const int32_t *n_tok
         case 642: launch_main_g<64, 2>(G, form, rs.share, gm, rows_z, s, a); break;
         case 644: launch_main_g<64, 4>(G, form, rs.share, gm, rows_z, s, a); break;
     }
+    if (whole) return hipGetLastError() != hipSuccess ? WUSHKV_ELAUNCH : WUSHKV_OK;  // (the output is written)
     if (step != nullptr) {
         if (hipGetLastError() != hipSuccess) return WUSHKV_ELAUNCH;
         return wushkv_step_finish(c, step->n_new, part, out, G, p.n_splits, p.n_page_splits, a.runs, s);
