@@ -417,22 +417,27 @@ def wushkv_dequant(cache: WushKVCache, b: int, start: int, count: int, k_out=Non
     return k_out, v_out
 
 
-def _check(cache, t, name, dtype, shape, optional=False):
+def _check(cache, t, name, dtype, shape):
     """A contiguous tensor of this type and shape on the cache's device."""
-    if t is None and optional:
-        return
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, list(shape)))
-    if t.device != cache.pages.device:
+    if t.get_device() != cache.pages.get_device():
         raise ValueError("%s is not on the cache's device" % name)
 
 
 def _launch_stream(cache, stream):
     """The stream handle of a call on the cache's device, which has to be the
     current one."""
-    if cache.pages.device.index != _torch().cuda.current_device():
+    torch = _torch()
+    current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)()
+    if cache.pages.get_device() != current:
         raise ValueError("the cache's device is not the current one")
-    return _stream_handle(stream)
+    if stream is not None:
+        if stream.device_index != current:
+            raise ValueError("the stream is not on the cache's device")
+        return stream.cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(current) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _on_stream(t, stream):
@@ -448,7 +453,8 @@ def wushkv_page_bounds(cache: WushKVCache, bounds: WushKVBounds, since=None, max
     [batch] on the device; None: of all complete pages), at most ``max_new``
     (by default max_pages) a sequence."""
     torch = _torch()
-    _check(cache, since, "since", torch.int32, (cache.batch,), True)
+    if since is not None:
+        _check(cache, since, "since", torch.int32, (cache.batch,))
     st = _lib.lib().wushkv_page_bounds(
         ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(since),
         cache.max_pages if max_new is None else operator.index(max_new), _launch_stream(cache, stream))
@@ -472,24 +478,27 @@ def wushkv_select_pages(cache: WushKVCache, bounds: WushKVBounds, q, t_k_inv, to
     n_q = q.shape[1] if q.dim() == 3 else 0
     _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
     _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
-    _check(cache, scores, "scores", torch.float32, (b, hk, cache.max_pages), True)
+    if scores is not None:
+        _check(cache, scores, "scores", torch.float32, (b, hk, cache.max_pages))
     if max_seq_len is None:
         max_seq_len = cache.max_seq_len
-    need = wushkv_select_workspace_bytes(cache, n_q, operator.index(max_seq_len), top_k)
+    max_seq_len = operator.index(max_seq_len)
     handle = _launch_stream(cache, stream)
-    if need:  # (otherwise the call says what is wrong)
-        if sel is None:
-            sel = _on_stream(torch.empty(b, hk, top_k + 1, dtype=torch.int32, device=q.device), stream)
-        if n_sel is None:
-            n_sel = _on_stream(torch.empty(b, hk, dtype=torch.int32, device=q.device), stream)
-        if workspace is None:
-            workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
-        _check(cache, sel, "sel", torch.int32, (b, hk, top_k + 1))
-        _check(cache, n_sel, "n_sel", torch.int32, (b, hk))
+    if workspace is None:
+        need = wushkv_select_workspace_bytes(cache, n_q, max_seq_len, top_k)
+        if need == 0:
+            raise WushKVError(_lib.EINVAL, "wushkv_select_workspace_bytes")
+        workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+    shape = (b, hk, top_k + 1)
+    if sel is None:
+        sel = _on_stream(torch.empty(shape, dtype=torch.int32, device=q.device), stream)
+    if n_sel is None:
+        n_sel = _on_stream(torch.empty(b, hk, dtype=torch.int32, device=q.device), stream)
+    _check(cache, sel, "sel", torch.int32, shape)
+    _check(cache, n_sel, "n_sel", torch.int32, (b, hk))
     st = _lib.lib().wushkv_select_pages(
-        ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(q), n_q, operator.index(max_seq_len),
-        _ptr(t_k_inv), top_k, _ptr(sel), _ptr(n_sel), _ptr(scores), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), handle)
+        ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(q), n_q, max_seq_len, _ptr(t_k_inv), top_k,
+        _ptr(sel), _ptr(n_sel), _ptr(scores), _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
     check(st, "wushkv_select_pages")
     return sel, n_sel
 
@@ -536,8 +545,9 @@ def wushkv_assign_pages(cache: WushKVCache, pool: WushKVPool, source=None, reach
     or -1 minus that where source[b] was refused."""
     torch = _torch()
     shape = (cache.batch,)
-    _check(cache, source, "source", torch.int32, shape, True)
-    _check(cache, reach, "reach", torch.int32, shape, True)
+    for t, name in ((source, "source"), (reach, "reach")):
+        if t is not None:
+            _check(cache, t, name, torch.int32, shape)
     handle = _launch_stream(cache, stream)
     if status is None:
         status = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
