@@ -38,14 +38,67 @@ __device__ __forceinline__ int32_t complete_pages(const int32_t *seq_len, const 
     return q > s_sink ? min((q - s_sink) / kPage, max_pages) : 0;
 }
 
+// Four values a and four c of a lane: a becomes op(a, the partner's a) in the
+// banks (groups of four lanes) A of a row and op(c, the partner's c) in the
+// others, the partner being the lane that CTRL names: half of an exchange that
+// leaves each lane half of the values, reduced over both lanes.  (A DPP operand
+// must not have been written in the two instructions before.)
+#define WUSHKV_HALVE(OP, CTRL, A, C, a, c)                                                       \
+    asm volatile("s_nop 1\n\t"                                                                  \
+                 OP " %0, %0, %0 " CTRL " row_mask:0xf bank_mask:" A "\n\t"                      \
+                 OP " %1, %1, %1 " CTRL " row_mask:0xf bank_mask:" A "\n\t"                      \
+                 OP " %2, %2, %2 " CTRL " row_mask:0xf bank_mask:" A "\n\t"                      \
+                 OP " %3, %3, %3 " CTRL " row_mask:0xf bank_mask:" A "\n\t"                      \
+                 OP " %0, %4, %4 " CTRL " row_mask:0xf bank_mask:" C "\n\t"                      \
+                 OP " %1, %5, %5 " CTRL " row_mask:0xf bank_mask:" C "\n\t"                      \
+                 OP " %2, %6, %6 " CTRL " row_mask:0xf bank_mask:" C "\n\t"                      \
+                 OP " %3, %7, %7 " CTRL " row_mask:0xf bank_mask:" C                              \
+                 : "+v"((a)[0]), "+v"((a)[1]), "+v"((a)[2]), "+v"((a)[3])                        \
+                 : "v"((c)[0]), "v"((c)[1]), "v"((c)[2]), "v"((c)[3]))
+
+// The least and the largest of 32 values over the 16 lanes of a row: lane n ends
+// with those of values 2 n and 2 n + 1 (x[0], x[1]).  Four exchanges, with lanes
+// n ^ 8, 7 - n (within eight), n ^ 2 and n ^ 1, each with half of the values
+// that are left.
+template <bool MAX>
+__device__ __forceinline__ void row_halves(float (&x)[32], int n)
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        if constexpr (MAX) WUSHKV_HALVE("v_max_f32_dpp", "row_ror:8", "0x3", "0xc", x + i, x + 16 + i);
+        else WUSHKV_HALVE("v_min_f32_dpp", "row_ror:8", "0x3", "0xc", x + i, x + 16 + i);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        if constexpr (MAX) WUSHKV_HALVE("v_max_f32_dpp", "row_half_mirror", "0x5", "0xa", x + i, x + 8 + i);
+        else WUSHKV_HALVE("v_min_f32_dpp", "row_half_mirror", "0x5", "0xa", x + i, x + 8 + i);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool up = (n & 2) != 0;
+        const float keep = up ? x[4 + i] : x[i], other = dpp<0x4E>(up ? x[i] : x[4 + i]);
+        x[i] = MAX ? fmaxf(keep, other) : fminf(keep, other);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool up = (n & 1) != 0;
+        const float keep = up ? x[2 + i] : x[i], other = dpp<0xB1>(up ? x[i] : x[2 + i]);
+        x[i] = MAX ? fmaxf(keep, other) : fminf(keep, other);
+    }
+}
+
 // Lane (j, n) of the wave holds channels 32 j .. 32 j + 31 of tokens 4 n ..
-// 4 n + 3 (the page layout); with d = 64 the upper half repeats the lower.
+// 4 n + 3 (the page layout); with d = 64 the upper half repeats the lower.  A code
+// masked where it stands in a half word, in fields F = 0 .. 6 of it, is the fp16
+// subnormal c 2^(F-24): times scale 2^(24-F), one mixed-precision fma gives
+// scale c + zero, rounded once, without any conversion.
 template <int D, int BITS>
 __global__ void __launch_bounds__(256) page_bounds_kernel(BoundsArgs a)
 {
     using L = Layout<D, BITS>;
     constexpr int kWords = L::kKWordsPerLane;     // 8 (2-bit) or 16 (4-bit)
     constexpr int kSpan = L::kCodesPerWord;       // channels per word
+    constexpr int kFields = 8 / BITS;             // fields of half of a half word
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t b = blockIdx.x / a.blocks;
     const int32_t item = (blockIdx.x % a.blocks) * 4 + wave;  // (new page, kv head)
@@ -61,58 +114,54 @@ __global__ void __launch_bounds__(256) page_bounds_kernel(BoundsArgs a)
 #pragma unroll
     for (int i = 0; i < kWords / 4; ++i) w[i] = *reinterpret_cast<const u32x4 *>(pg + 4 * L::k_word(src, 4 * i));
     const u32x4 par = *reinterpret_cast<const u32x4 *>(pg + L::kParamOffset + 16 * n);
-    float lo[32], hi[32];
-    bool odd = false;  // a parameter that is not finite
+    float sc[4][kFields], zr[4];  // scale 2^(24 - F), zero
+    bool odd = false;             // a parameter that is not finite
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         odd |= (par[t] & 0x7C00u) == 0x7C00u || (par[t] & 0x7C000000u) == 0x7C000000u;
-        const float sc = f16_bits_to_f32(par[t] & 0xFFFFu), zr = f16_bits_to_f32(par[t] >> 16);
+        zr[t] = f16_bits_to_f32(par[t] >> 16);
 #pragma unroll
-        for (int i = 0; i < BITS; ++i) {
-            const uint32_t x = w[(BITS * t + i) / 4][(BITS * t + i) % 4];
+        for (int f = 0; f < kFields; ++f) sc[t][f] = f16_bits_to_f32(par[t] & 0xFFFFu) * (16777216.0f / (1 << (BITS * f)));
+    }
+    float lo[32], hi[32];
 #pragma unroll
-            for (int e = 0; e < kSpan; ++e) {
-                const int bit = 2 * BITS * (e % (kSpan / 2)) + BITS * (e / (kSpan / 2));
-                const float v = fmaf(sc, (float)((x >> bit) & ((1u << BITS) - 1u)), zr);
-                const int ch = kSpan * i + e;
-                lo[ch] = t == 0 ? v : fminf(lo[ch], v);
-                hi[ch] = t == 0 ? v : fmaxf(hi[ch], v);
+    for (int i = 0; i < BITS; ++i)  // the word of a token
+#pragma unroll
+        for (int byte = 0; byte < 2; ++byte)
+#pragma unroll
+            for (int f = 0; f < kFields; ++f) {
+                // field 8 byte + BITS f of both half words: element e and e + kSpan / 4
+                const int field = 8 * byte + BITS * f;
+                const int e = (f & 1) * (kSpan / 2) + field / (2 * BITS);
+                const uint32_t mask = ((1u << BITS) - 1u) * 0x00010001u << (BITS * f);
+                float x[4], y[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const uint32_t v = (w[(BITS * t + i) / 4][(BITS * t + i) % 4] >> (8 * byte)) & mask;
+                    x[t] = fmaf(sc[t][f], f16_bits_to_f32(v & 0xFFFFu), zr[t]);
+                    y[t] = fmaf(sc[t][f], f16_bits_to_f32(v >> 16), zr[t]);
+                }
+                const int ch = kSpan * i + e, ch2 = ch + kSpan / 4;
+                lo[ch] = fminf(fminf(fminf(x[0], x[1]), x[2]), x[3]);
+                hi[ch] = fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), x[3]);
+                lo[ch2] = fminf(fminf(fminf(y[0], y[1]), y[2]), y[3]);
+                hi[ch2] = fmaxf(fmaxf(fmaxf(y[0], y[1]), y[2]), y[3]);
             }
-        }
-    }
-    // over the tokens: the 16 lanes of a row
-    float top = 0.0f;
-#pragma unroll
-    for (int ch = 0; ch < 32; ++ch) {
-        float x = lo[ch], y = hi[ch];
-        x = fminf(x, dpp<0xB1>(x)); y = fmaxf(y, dpp<0xB1>(y));
-        x = fminf(x, dpp<0x4E>(x)); y = fmaxf(y, dpp<0x4E>(y));
-        x = fminf(x, dpp<0x124>(x)); y = fmaxf(y, dpp<0x124>(y));
-        x = fminf(x, dpp<0x128>(x)); y = fmaxf(y, dpp<0x128>(y));
-        lo[ch] = x;
-        hi[ch] = y;
-        top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
-    }
+    // over the tokens; lane n of a row then finishes channels 2 n and 2 n + 1 of its 32
+    row_halves<false>(lo, n);
+    row_halves<true>(hi, n);
     const bool any_odd = __any(odd);
-    top = wave_max(any_odd ? 0.0f : top);
+    const float top = any_odd ? 0.0f
+                              : wave_max(fmaxf(fmaxf(fabsf(lo[0]), fabsf(hi[0])), fmaxf(fabsf(lo[1]), fabsf(hi[1]))));
     const float s = any_odd ? INFINITY : top / 126.0f;
-    // lane n of a row finishes channels 2 n and 2 n + 1 of its 32
-    float l2[2] = {lo[0], lo[1]}, h2[2] = {hi[0], hi[1]};
-#pragma unroll
-    for (int i = 1; i < 16; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            l2[e] = n == i ? lo[2 * i + e] : l2[e];
-            h2[e] = n == i ? hi[2 * i + e] : h2[e];
-        }
     int c[2] = {0, 0}, r[2] = {0, 0};
     if (top > 0.0f) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float mid = rintf(((l2[e] + h2[e]) * 0.5f) / s);
+            const float mid = rintf(((lo[e] + hi[e]) * 0.5f) / s);
             const float ms = mid * s;
             c[e] = (int)mid;
-            r[e] = (int)fminf(ceilf(fmaxf(h2[e] - ms, ms - l2[e]) / s), 127.0f);
+            r[e] = (int)fminf(ceilf(fmaxf(hi[e] - ms, ms - lo[e]) / s), 127.0f);
         }
     }
     if (lane >= L::kKLanes) return;
