@@ -4,18 +4,23 @@
 // the result depends on the arguments alone.
 //
 // assign, up to three launches:
-//   assign_rows_kernel   (with a source map) one thread per (sequence, logical
-//                        page): drops the references of freed and forked rows,
-//                        writes the forks' shared entries and counts them.
+//   assign_rows_kernel   (a source map over more than a few entries) one thread
+//                        per (sequence, logical page): drops the references of
+//                        freed and forked rows, writes the forks' shared entries
+//                        and counts them.
 //   assign_pages_kernel  one workgroup: what every sequence needs, a prefix sum
 //                        over the sequences, then the free pages in order from
-//                        pool->low on, each to the sequence its rank falls to.
-//   assign_copy_kernel   (with a source map) the forks' windows and the page
-//                        being filled, 32 KB a workgroup.
-// compact, three launches:
-//   compact_count_kernel used pages per block of kBlock references.
+//                        pool->low on, each to the sequence its rank falls to; the
+//                        others copy the forks' windows.
+//   assign_copy_kernel   (with a source map) the forks' pages being filled.
+// compact, two launches, three for large pools:
+//   compact_count_kernel (large pools) used pages per block of kBlock references.
 //   compact_plan_kernel  ranks: free pages below n and used ones from n on.
 //   compact_move_kernel  the pages, the boxes, references and table entries.
+// What bounds them: small calls are launches (about 4 us each) and the one
+// workgroup's dependent reads; large ones are copies, 64 sequences with 56 forks
+// 17.3 us a call for 46 MB written (their sources are read from the caches), 1280
+// moved pages of 36 KB with their boxes 28 us, 5.3 TB/s read and written.
 #include "common.h"
 #include "merge.h"
 
@@ -23,6 +28,10 @@ namespace wushkv {
 
 constexpr int kMaxAssignBatch = 16384;  // the sequences' starts and bases stay in LDS
 constexpr int kAssignThreads = 1024;
+constexpr int kFewSequences = 1024;     // the same, in less LDS
+// Table entries up to which the one workgroup goes through them itself: 248
+// entries 12.8 us a call, with a launch for them 14.8; 8064, 48.8 and 26.2.
+constexpr int kOneAssign = 1024;
 
 struct AssignArgs {
     uint8_t *pages;
@@ -34,7 +43,7 @@ struct AssignArgs {
     int32_t *status;
     int32_t batch, n_kv, s_sink, max_pages, n_pages;
     int64_t page_units, win_units;  // 16-byte units of a page (all heads) and of one window of a sequence
-    int32_t row_blocks, copy_blocks;
+    int32_t row_blocks, win_blocks, copy_blocks;  // of a row, a window, a page
 };
 
 enum { kKeep = 0, kFree = 1, kFork = 2, kRefused = 3 };
@@ -64,13 +73,12 @@ __device__ __forceinline__ int32_t held_pages(const AssignArgs &a, int32_t b)
     return min(max(a.held[b], 0), a.max_pages);
 }
 
-__global__ void __launch_bounds__(256) assign_rows_kernel(AssignArgs a)
+// Entry lp of sequence b's row, if that is freed or forked.
+__device__ __forceinline__ void assign_entry(const AssignArgs &a, int32_t b, int32_t lp)
 {
-    const int32_t b = blockIdx.x / a.row_blocks;
-    const int32_t lp = (blockIdx.x % a.row_blocks) * 256 + threadIdx.x;
     int32_t s;
     const int kind = source_kind(a, b, s);
-    if ((kind != kFree && kind != kFork) || lp >= a.max_pages) return;
+    if (kind != kFree && kind != kFork) return;
     int32_t *row = a.page_table + (int64_t)b * a.max_pages;
     const int32_t old = row[lp];
     int32_t now = -1;
@@ -82,6 +90,17 @@ __global__ void __launch_bounds__(256) assign_rows_kernel(AssignArgs a)
     }
     if (now >= 0 && now < a.n_pages) atomicAdd(a.refs + now, 1);
     row[lp] = now;
+}
+
+__global__ void __launch_bounds__(256) assign_rows_kernel(AssignArgs a)
+{
+    const int32_t lp = (blockIdx.x % a.row_blocks) * 256 + threadIdx.x;
+    if (lp < a.max_pages) assign_entry(a, blockIdx.x / a.row_blocks, lp);
+}
+
+__device__ __forceinline__ int32_t load_agent(const int32_t *p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // Exclusive prefix sum over the workgroup's threads, and the total.
@@ -102,11 +121,48 @@ __device__ __forceinline__ int32_t block_scan(int32_t x, int32_t *sums, int32_t 
     return before + in - x;
 }
 
+// Up to 2 NT 16-byte units, by NT threads.  The stores are nontemporal: lines
+// that nothing reads soon, kept, cost the caches twice the time (111 windows and
+// 56 pages of 56 forks 29.3 us, so 14.6; 1280 moved pages 56.7, so 28.3), and two
+// units a thread are the best of 1 to 16 (30.3, 28.3, 38.4, 46.6, 33.2).
+template <int NT>
+__device__ __forceinline__ void copy_units(const u32x4 *src, u32x4 *dst, int64_t n)
+{
+    u32x4 v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (NT * i + threadIdx.x < n) v[i] = src[NT * i + threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (NT * i + threadIdx.x < n) __builtin_nontemporal_store(v[i], dst + NT * i + threadIdx.x);
+}
+constexpr int kCopyUnits = 512;  // of 256 threads
+
+// The first workgroup hands out pages; the others, if any, copy the forks'
+// windows meanwhile (nothing that the first one writes is read for that).
+// ROWS: the first one goes through the table's entries too, before anything else.
+template <bool ROWS, int MAX_BATCH>
 __global__ void __launch_bounds__(kAssignThreads) assign_pages_kernel(AssignArgs a)
 {
-    __shared__ int32_t start[kMaxAssignBatch + 1], base[kMaxAssignBatch];
+    __shared__ int32_t start[MAX_BATCH + 1], base[MAX_BATCH];
     __shared__ int32_t sums[kAssignThreads / 64];
     const int tid = threadIdx.x;
+    if (blockIdx.x > 0) {
+        for (int64_t w = blockIdx.x - 1; w < (int64_t)a.batch * 2 * a.win_blocks; w += gridDim.x - 1) {
+            const int32_t b = (int32_t)(w / (2 * a.win_blocks)), part = (int32_t)(w % (2 * a.win_blocks));
+            int32_t s;
+            if (source_kind(a, b, s) != kFork) continue;
+            const int64_t at = (int64_t)(part % a.win_blocks) * 2 * kAssignThreads;
+            uint16_t *win = part < a.win_blocks ? a.win_k : a.win_v;
+            copy_units<kAssignThreads>(reinterpret_cast<const u32x4 *>(win) + s * a.win_units + at,
+                                       reinterpret_cast<u32x4 *>(win) + b * a.win_units + at, a.win_units - at);
+        }
+        return;
+    }
+    if constexpr (ROWS) {
+        for (int32_t i = tid; i < a.batch * a.max_pages; i += kAssignThreads) assign_entry(a, i / a.max_pages, i % a.max_pages);
+        __syncthreads();  // (the references are read below, at the scope of their atomics)
+    }
     // what each sequence needs: pages base .. base + need - 1 of its row
     int32_t total = 0;
     for (int32_t b0 = 0; b0 < a.batch; b0 += kAssignThreads) {
@@ -134,13 +190,18 @@ __global__ void __launch_bounds__(kAssignThreads) assign_pages_kernel(AssignArgs
     }
     if (tid == 0) start[a.batch] = total;
     // the free pages in order: the i-th goes to the sequence whose needs span i
-    const int32_t first = total > 0 ? max(a.low[0], 0) : 0;
+    const int32_t first = total > 0 ? max(load_agent(a.low), 0) : 0;
     __syncthreads();  // (and the starts)
     int32_t found = 0;
     for (int64_t p0 = first & ~3; p0 < a.n_pages && found < total; p0 += 4 * kAssignThreads) {
         const int64_t p = p0 + 4 * tid;
         int4 r = make_int4(1, 1, 1, 1);
-        if (p + 3 < a.n_pages) {
+        if (ROWS) {
+            if (p < a.n_pages) r.x = load_agent(a.refs + p);
+            if (p + 1 < a.n_pages) r.y = load_agent(a.refs + p + 1);
+            if (p + 2 < a.n_pages) r.z = load_agent(a.refs + p + 2);
+            if (p + 3 < a.n_pages) r.w = load_agent(a.refs + p + 3);
+        } else if (p + 3 < a.n_pages) {
             r = *reinterpret_cast<const int4 *>(a.refs + p);
         } else {
             if (p < a.n_pages) r.x = a.refs[p];
@@ -188,46 +249,24 @@ __global__ void __launch_bounds__(kAssignThreads) assign_pages_kernel(AssignArgs
     }
 }
 
-// 16-byte units [at, at + n) of a copy, 256 threads, eight loads in flight each.
-constexpr int kCopyUnits = 2048;
-__device__ __forceinline__ void copy_units(const uint4 *src, uint4 *dst, int64_t n)
-{
-    uint4 v[kCopyUnits / 256];
-#pragma unroll
-    for (int i = 0; i < kCopyUnits / 256; ++i)
-        if (256 * i + threadIdx.x < n) v[i] = src[256 * i + threadIdx.x];
-#pragma unroll
-    for (int i = 0; i < kCopyUnits / 256; ++i)
-        if (256 * i + threadIdx.x < n) dst[256 * i + threadIdx.x] = v[i];
-}
-
 __global__ void __launch_bounds__(256) assign_copy_kernel(AssignArgs a)
 {
     const int32_t b = blockIdx.x / a.copy_blocks;
     int32_t s;
     if (source_kind(a, b, s) != kFork) return;
-    // blocks of one window, then of the other, then of the page
-    int64_t at = (int64_t)(blockIdx.x % a.copy_blocks) * kCopyUnits;
-    const int64_t win = (a.win_units + kCopyUnits - 1) / kCopyUnits * kCopyUnits;
-    if (at < 2 * win) {
-        uint16_t *w = at < win ? a.win_k : a.win_v;
-        if (at >= win) at -= win;
-        const uint4 *u = reinterpret_cast<const uint4 *>(w);
-        copy_units(u + s * a.win_units + at, reinterpret_cast<uint4 *>(w) + b * a.win_units + at, a.win_units - at);
-        return;
-    }
-    at -= 2 * win;
+    const int64_t at = (int64_t)(blockIdx.x % a.copy_blocks) * kCopyUnits;
     const int32_t q = quantised(a, s), lp = q / kPage;
     if (q % kPage == 0 || lp >= a.max_pages || lp >= a.held[b]) return;
     const int32_t from = a.page_table[(int64_t)s * a.max_pages + lp], to = a.page_table[(int64_t)b * a.max_pages + lp];
     if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) return;
-    uint4 *pool = reinterpret_cast<uint4 *>(a.pages);
-    copy_units(pool + from * a.page_units + at, pool + to * a.page_units + at, a.page_units - at);
+    u32x4 *pool = reinterpret_cast<u32x4 *>(a.pages);
+    copy_units<256>(pool + from * a.page_units + at, pool + to * a.page_units + at, a.page_units - at);
 }
 
 // ------------------------------------------------------------------ compact
 
 constexpr int kBlock = 4096;  // references per workgroup of the count and the plan
+constexpr int kOwnCount = 8;  // blocks up to which the plan counts them itself
 
 struct CompactArgs {
     uint8_t *pages;
@@ -252,62 +291,84 @@ __device__ __forceinline__ int32_t block_sum(int32_t x, int32_t *sums)
     return total;
 }
 
-__global__ void __launch_bounds__(256) compact_count_kernel(CompactArgs a)
+// References p .. p + 3, 0 behind the last page.
+__device__ __forceinline__ int4 four_refs(const CompactArgs &a, int64_t p)
 {
-    __shared__ int32_t sums[4];
-    int32_t n = 0;
-    const int64_t p0 = (int64_t)blockIdx.x * kBlock;
-#pragma unroll
-    for (int i = 0; i < kBlock / 256; ++i) {
-        const int64_t p = p0 + 256 * i + threadIdx.x;
-        if (p < a.n_pages) n += a.refs[p] > 0;
-    }
-    n = block_sum(n, sums);
+    int4 r = make_int4(0, 0, 0, 0);
+    if (p + 3 < a.n_pages) return *reinterpret_cast<const int4 *>(a.refs + p);
+    if (p < a.n_pages) r.x = a.refs[p];
+    if (p + 1 < a.n_pages) r.y = a.refs[p + 1];
+    if (p + 2 < a.n_pages) r.z = a.refs[p + 2];
+    return r;
+}
+__device__ __forceinline__ int32_t in_use(const int4 &r) { return (r.x > 0) + (r.y > 0) + (r.z > 0) + (r.w > 0); }
+
+__global__ void __launch_bounds__(kBlock / 4) compact_count_kernel(CompactArgs a)
+{
+    __shared__ int32_t sums[kBlock / 256];
+    const int32_t n = block_sum(in_use(four_refs(a, (int64_t)blockIdx.x * kBlock + 4 * threadIdx.x)), sums);
     if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
 }
 
-__global__ void __launch_bounds__(256) compact_plan_kernel(CompactArgs a)
+// COUNTED: the blocks' counts are there; otherwise every workgroup counts the
+// (few) blocks itself.
+template <bool COUNTED>
+__global__ void __launch_bounds__(kBlock / 4) compact_plan_kernel(CompactArgs a)
 {
-    __shared__ int32_t sums[4];
+    __shared__ int32_t sums[kBlock / 256];
     const int tid = threadIdx.x;
     const int32_t mine = blockIdx.x;
     // pages in use: in all, before this block, and below n
     int32_t all = 0, before = 0;
-    for (int32_t i = tid; i < a.n_blocks; i += 256) {
-        const int32_t v = a.counts[i];
-        all += v;
-        if (i < mine) before += v;
+    if constexpr (COUNTED) {
+        for (int32_t i = tid; i < a.n_blocks; i += kBlock / 4) {
+            const int32_t v = a.counts[i];
+            all += v;
+            if (i < mine) before += v;
+        }
+    } else {
+        for (int32_t i = 0; i < a.n_blocks; ++i) {
+            const int32_t v = in_use(four_refs(a, (int64_t)i * kBlock + 4 * tid));
+            all += v;
+            if (i < mine) before += v;
+        }
     }
     const int32_t live = block_sum(all, sums);
     before = block_sum(before, sums);
-    int32_t below = 0;
-    for (int32_t i = tid; i < live / kBlock; i += 256) below += a.counts[i];
     // (references below n keep their values in this launch, also in place)
-    for (int64_t p = (int64_t)live / kBlock * kBlock + tid; p < live; p += 256) below += a.refs[p] > 0;
+    int32_t below = 0;
+    const int32_t whole = live / kBlock;
+    if constexpr (COUNTED) {
+        for (int32_t i = tid; i < whole; i += kBlock / 4) below += a.counts[i];
+    }
+    for (int64_t p = (COUNTED ? (int64_t)whole * kBlock : 0) + tid; p < live; p += kBlock / 4) below += a.refs[p] > 0;
     below = block_sum(below, sums);
     if (mine == 0 && tid == 0) {
         a.head[0] = live;
         a.head[1] = live - below;
         if (a.live_out != nullptr) a.live_out[0] = live;
     }
-    for (int i = 0; i < kBlock / 256; ++i) {
-        const int64_t p = (int64_t)mine * kBlock + 256 * i + tid;
-        const int32_t r = p < a.n_pages ? a.refs[p] : 0;
-        int32_t sum;
-        const int32_t at = before + block_scan(r > 0, sums, sum);  // pages in use before p
-        before += sum;
-        if (p >= a.n_pages) continue;
+    const int64_t p0 = (int64_t)mine * kBlock + 4 * tid;
+    const int4 r = four_refs(a, p0);
+    int32_t sum;
+    int32_t at = before + block_scan(in_use(r), sums, sum);  // pages in use before p
+    const int32_t v[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int64_t p = p0 + e;
+        if (p >= a.n_pages) break;
         if (p < live) {
-            if (r > 0) a.refs_out[p] = r;
+            if (v[e] > 0) a.refs_out[p] = v[e];
             else a.hole[p - at] = (int32_t)p;
         } else {
-            if (r > 0) {
+            if (v[e] > 0) {
                 a.mover[at - below] = (int32_t)p;
-                a.mover_refs[at - below] = r;
+                a.mover_refs[at - below] = v[e];
             }
-            a.rank[p] = r > 0 ? at - below : -1;
+            a.rank[p] = v[e] > 0 ? at - below : -1;
             a.refs_out[p] = 0;
         }
+        at += v[e] > 0;
     }
 }
 
@@ -334,14 +395,14 @@ __global__ void __launch_bounds__(256) compact_move_kernel(CompactArgs a)
         const int32_t i = (int32_t)(w / each), part = (int32_t)(w % each);
         const int64_t from = a.mover[i], to = a.hole[i];
         if (part < per) {
-            uint4 *pool = reinterpret_cast<uint4 *>(a.pages);
+            u32x4 *pool = reinterpret_cast<u32x4 *>(a.pages);
             const int64_t at = (int64_t)part * kCopyUnits;
-            copy_units(pool + from * a.page_units + at, pool + to * a.page_units + at, a.page_units - at);
+            copy_units<256>(pool + from * a.page_units + at, pool + to * a.page_units + at, a.page_units - at);
             continue;
         }
         if (tid == 0) a.refs_out[to] = a.mover_refs[i];
         if (a.codes == nullptr) continue;
-        uint4 *codes = reinterpret_cast<uint4 *>(a.codes);
+        u32x4 *codes = reinterpret_cast<u32x4 *>(a.codes);
         for (int64_t u = tid; u < a.code_units; u += 256) codes[to * a.code_units + u] = codes[from * a.code_units + u];
         for (int32_t h = tid; h < a.n_kv; h += 256) a.scales[(int64_t)h * a.n_pages + to] = a.scales[(int64_t)h * a.n_pages + from];
     }
@@ -394,16 +455,24 @@ extern "C" int wushkv_assign_pages(const wushkv_cache *c, const wushkv_pool *poo
     a.page_units = (int64_t)c->n_kv_heads * (int64_t)(wushkv_page_bytes(c->head_dim, c->bits) / 16);
     a.win_units = (int64_t)c->n_kv_heads * c->win_slots * c->head_dim / 8;
     const int64_t row_blocks = (a.max_pages + 255) / 256;
-    const int64_t copy_blocks = 2 * ((a.win_units + kCopyUnits - 1) / kCopyUnits) +
-                                (paged ? (a.page_units + kCopyUnits - 1) / kCopyUnits : 0);
-    if (row_blocks * c->batch > 0x7FFFFFFF || copy_blocks * c->batch > 0x7FFFFFFF) return WUSHKV_EUNSUPPORTED;
+    const int64_t win_blocks = (a.win_units + 2 * kAssignThreads - 1) / (2 * kAssignThreads);
+    const int64_t copy_blocks = paged ? (a.page_units + kCopyUnits - 1) / kCopyUnits : 0;
+    if (win_blocks > 0x3FFFFFFF || copy_blocks * c->batch > 0x7FFFFFFF) return WUSHKV_EUNSUPPORTED;
     a.row_blocks = (int32_t)row_blocks;
+    a.win_blocks = (int32_t)win_blocks;
     a.copy_blocks = (int32_t)copy_blocks;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (source != nullptr && row_blocks > 0)
+    const bool few = c->batch <= kFewSequences;
+    const int64_t entries = (int64_t)c->batch * a.max_pages, copies = 2 * win_blocks * c->batch;
+    const bool rows = source != nullptr && entries <= kOneAssign;
+    const dim3 grid(source == nullptr ? 1u : 1u + (unsigned)(copies < 2048 ? copies : 2048)), threads(kAssignThreads);
+    if (source != nullptr && !rows)
         launch("assign_rows_kernel", assign_rows_kernel, dim3((unsigned)(row_blocks * c->batch)), dim3(256), s, a);
-    launch("assign_pages_kernel", assign_pages_kernel, dim3(1), dim3(kAssignThreads), s, a);
-    if (source != nullptr)
+    if (rows && few) launch("assign_pages_kernel", assign_pages_kernel<true, kFewSequences>, grid, threads, s, a);
+    else if (rows) launch("assign_pages_kernel", assign_pages_kernel<true, kMaxAssignBatch>, grid, threads, s, a);
+    else if (few) launch("assign_pages_kernel", assign_pages_kernel<false, kFewSequences>, grid, threads, s, a);
+    else launch("assign_pages_kernel", assign_pages_kernel<false, kMaxAssignBatch>, grid, threads, s, a);
+    if (source != nullptr && copy_blocks > 0)
         launch("assign_copy_kernel", assign_copy_kernel, dim3((unsigned)(copy_blocks * c->batch)), dim3(256), s, a);
     if (hipGetLastError() != hipSuccess) return WUSHKV_ELAUNCH;
     return WUSHKV_OK;
@@ -466,8 +535,13 @@ extern "C" int wushkv_compact_pages(const wushkv_cache *c, const wushkv_pool *po
     const int64_t copies = (int64_t)(a.n_pages / 2) * each;
     const unsigned move_blocks = (unsigned)(a.table_blocks + (copies < 2048 ? copies : 2048));
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    launch("compact_count_kernel", compact_count_kernel, dim3((unsigned)a.n_blocks), dim3(256), s, a);
-    launch("compact_plan_kernel", compact_plan_kernel, dim3((unsigned)a.n_blocks), dim3(256), s, a);
+    const dim3 blocks((unsigned)a.n_blocks), threads(kBlock / 4);
+    if (a.n_blocks <= kOwnCount) {
+        launch("compact_plan_kernel", compact_plan_kernel<false>, blocks, threads, s, a);
+    } else {
+        launch("compact_count_kernel", compact_count_kernel, blocks, threads, s, a);
+        launch("compact_plan_kernel", compact_plan_kernel<true>, blocks, threads, s, a);
+    }
     launch("compact_move_kernel", compact_move_kernel, dim3(move_blocks), dim3(256), s, a);
     if (hipGetLastError() != hipSuccess) return WUSHKV_ELAUNCH;
     return WUSHKV_OK;
