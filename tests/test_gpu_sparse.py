@@ -125,15 +125,65 @@ def test_grids_of_rounds_and_long_lists(gpu, batch, hk, G, bits, width):
         return
     got = run(gpu, h, q, t, sel, n)
     pick = rng.choice(batch, 4, replace=False)
-    part = object.__new__(Host)
-    part.__dict__.update(h.__dict__)
-    part.b = 4
-    for name in ("seq_len", "quant_end", "table", "win_k", "win_v"):
-        setattr(part, name, getattr(h, name)[pick])
-    want, tol = pages_ref.attention(part, q[pick], t, sel[pick], n[pick], 1.0 / np.sqrt(128))
+    want, tol = pages_ref.attention(some(h, pick), q[pick], t, sel[pick], n[pick], 1.0 / np.sqrt(128))
     assert (np.abs(got[pick] - want).max(-1) <= tol).all()
     # the same call again: the same bits
     assert np.array_equal(run(gpu, h, q, t, sel, n), got)
+
+
+def some(host, pick):
+    """The state of some of a host's sequences."""
+    part = object.__new__(Host)
+    part.__dict__.update(host.__dict__)
+    part.b = len(pick)
+    for name in ("seq_len", "quant_end", "table", "win_k", "win_v"):
+        setattr(part, name, getattr(host, name)[pick])
+    return part
+
+
+@pytest.mark.parametrize("d,bits,G,slots", [(128, 2, 1, 64), (128, 4, 2, 64), (128, 2, 8, 128), (128, 4, 8, 64), (64, 2, 8, 64),
+                                            (64, 4, 2, 192), (128, 3, 4, 64)])
+def test_a_row_for_every_compute_unit(gpu, d, bits, G, slots):
+    """Batches whose rows are one workgroup's each, lists of no page to more
+    than there are."""
+    say("sparse, whole rows: d %d, %d-bit, G %d, %d slots" % (d, bits, G, slots))
+    rng = np.random.default_rng([d, bits, G, slots])
+    lens = rng.integers(0, 330, 150)
+    lens[:8] = [0, 1, 4, 5, 36, 45, 100, 329]
+    h = Host(rng, lens, 2, d, bits, win_slots=slots)
+    q = synth.to_bf16_bits(rng.standard_normal((h.b, 2 * G, d)))
+    t = pages_ref.transform(rng, 2, d)
+    pick = np.concatenate([np.arange(8), rng.choice(np.arange(8, 150), 5, replace=False)])
+    for width in (0, 3, 70):
+        sel, n = lists(rng, h, width) if width < 70 else (rng.integers(-1, 5, (h.b, 2, 70)).astype(np.int32),
+                                                          rng.integers(0, 80, (h.b, 2)).astype(np.int32))
+        got = run(gpu, h, q, t, sel, n)
+        want, tol = pages_ref.attention(some(h, pick), q[pick], t, sel[pick], n[pick], 1.0 / np.sqrt(d))
+        off = np.abs(got[pick] - want).max(-1)
+        say("  width %d: of its bound %.2f" % (width, (off / np.maximum(tol, 1e-30)).max()))
+        assert (off <= tol).all() and np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("batch,d,bits", [(2, 128, 4), (2, 64, 2), (140, 128, 2)])
+def test_large_value_scales(gpu, batch, d, bits):
+    """Values far larger in some pages than in others: weights times scales
+    beyond fp16 if they were lifted everywhere."""
+    rng = np.random.default_rng([batch, d, bits])
+    h = Host(rng, [700] * 2 + [50] * (batch - 2), 2, d, bits)
+    par = h.pages.shape[2] - 256
+    for lp, scale in ((1, 150.0), (4, 30000.0), (7, 127.0), (9, 60000.0)):
+        for b in range(2):
+            view = h.pages[h.table[b, lp], :, par:].view(np.float16).reshape(2, 64, 2)
+            view[:, :, 0] = scale
+            h.pages[h.table[b, lp], :, par:] = view.reshape(2, 128).view(np.uint8)
+    q = synth.to_bf16_bits(rng.standard_normal((h.b, 4, d)))
+    t = pages_ref.transform(rng, 2, d)
+    for _ in range(3):
+        sel, n = lists(rng, h, 10)
+        got = run(gpu, h, q, t, sel, n)
+        pick = np.arange(min(batch, 4))
+        want, tol = pages_ref.attention(some(h, pick), q[pick], t, sel[pick], n[pick], 1.0 / np.sqrt(d))
+        assert (np.abs(got[pick] - want).max(-1) <= tol).all()
 
 
 # ------------------------------------------------------------------ together
