@@ -227,7 +227,7 @@ __device__ __forceinline__ void stage_queries(const QueryIn<D, G, NT> &in, uint8
 // forms the same q~.  Every thread of the workgroup calls it after
 // stage_queries; it starts and ends with a barrier.
 template <int D, int G>
-__device__ void form_qt(const DecodeArgs &a, const QueryIn<D, G> &in, uint8_t *R, int tid)
+__device__ __forceinline__ void form_qt(const DecodeArgs &a, const QueryIn<D, G> &in, uint8_t *R, int tid)
 {
     using C = QueryIn<D, G>;
     const uint16_t *qs = reinterpret_cast<const uint16_t *>(R);
@@ -314,7 +314,7 @@ struct TColumns {
 // fp32, into R; starts and ends with a barrier); the products are summed in
 // the matrix unit's order, so q~ may differ from form_qt's in the last bits.
 template <int D, int G>
-__device__ void form_qt_mfma(const DecodeArgs &a, const TColumns<D> &tc, uint8_t *R, int tid)
+__device__ __forceinline__ void form_qt_mfma(const DecodeArgs &a, const TColumns<D> &tc, uint8_t *R, int tid)
 {
     constexpr int kSteps = TColumns<D>::kSteps;
     const uint16_t *qs = reinterpret_cast<const uint16_t *>(R);
@@ -358,7 +358,7 @@ __device__ void form_qt_mfma(const DecodeArgs &a, const TColumns<D> &tc, uint8_t
 // 32 j + 31 in its 32 bytes of a limb, one byte each (fp8) or six bits each
 // in the first 24 (fp6).
 template <int D, int BITS, int G, int NW = 4>
-__device__ void form_limbs(uint8_t *R, int tid)
+__device__ __forceinline__ void form_limbs(uint8_t *R, int tid)
 {
     using Q = QueryLds<D, G>;
     const int lane = tid & 63, wave = tid >> 6;
@@ -668,7 +668,7 @@ struct MainLds {
 // the windows and to tok (LDS: bf16 k~ [D], then v [D]).  Every thread of
 // the workgroup calls it; it ends with a barrier.
 template <int D>
-__device__ void step_token(const DecodeArgs &a, int b, int h, int32_t slot, uint16_t *tok, int tid)
+__device__ __forceinline__ void step_token(const DecodeArgs &a, int b, int h, int32_t slot, uint16_t *tok, int tid)
 {
     constexpr int kNtW = D / 64;
     constexpr int kC = D / 32;
