@@ -505,7 +505,8 @@ size_t wushkv_sparse_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads, i
 /*
  * A pool's bookkeeping, for caches whose sequences share one pool of pages.
  *   refs   int32 [n_pages]: page-table rows that hold the page; 0: free.  A page
- *          the caller adds a reference to is not handed out or freed.
+ *          the caller adds a reference to is not handed out or freed (a
+ *          compaction moves it like any other).
  *   held   int32 [batch]: pages sequence b holds: its page-table row is valid in
  *          [0, held[b]) and not read beyond.
  *   low    int32 [1]: no page below low[0] is free (0 is always right; kept so

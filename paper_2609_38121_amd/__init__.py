@@ -425,6 +425,18 @@ def _check(cache, t, name, dtype, shape):
         raise ValueError("%s is not on the cache's device" % name)
 
 
+def _check_parts(cache, bounds=None, pool=None, workspace=None):
+    """Boxes and a pool of this cache's sizes, a workspace on its device."""
+    if bounds is not None and (bounds.codes.shape != (cache.n_pages, cache.n_kv_heads, 2, cache.head_dim)
+                               or bounds.codes.get_device() != cache.pages.get_device()):
+        raise ValueError("bounds are not this cache's")
+    if pool is not None and (pool.refs.numel() != cache.n_pages or pool.held.numel() != cache.batch
+                             or pool.refs.get_device() != cache.pages.get_device()):
+        raise ValueError("pool is not this cache's")
+    if workspace is not None and (not workspace.is_contiguous() or workspace.get_device() != cache.pages.get_device()):
+        raise ValueError("workspace must be contiguous and on the cache's device")
+
+
 def _launch_stream(cache, stream):
     """The stream handle of a call on the cache's device, which has to be the
     current one."""
@@ -453,6 +465,7 @@ def wushkv_page_bounds(cache: WushKVCache, bounds: WushKVBounds, since=None, max
     [batch] on the device; None: of all complete pages), at most ``max_new``
     (by default max_pages) a sequence."""
     torch = _torch()
+    _check_parts(cache, bounds)
     if since is not None:
         _check(cache, since, "since", torch.int32, (cache.batch,))
     st = _lib.lib().wushkv_page_bounds(
@@ -476,6 +489,7 @@ def wushkv_select_pages(cache: WushKVCache, bounds: WushKVBounds, q, t_k_inv, to
     torch = _torch()
     b, hk, d, top_k = cache.batch, cache.n_kv_heads, cache.head_dim, operator.index(top_k)
     n_q = q.shape[1] if q.dim() == 3 else 0
+    _check_parts(cache, bounds, workspace=workspace)
     _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
     _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
     if scores is not None:
@@ -516,6 +530,7 @@ def wushkv_sparse_attention(cache: WushKVCache, q, t_k_inv, sel, n_sel, sm_scale
     b, hk, d = cache.batch, cache.n_kv_heads, cache.head_dim
     n_q = q.shape[1] if q.dim() == 3 else 0
     max_sel = sel.shape[2] if sel.dim() == 3 else 0
+    _check_parts(cache, workspace=workspace)
     _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
     _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
     _check(cache, sel, "sel", torch.int32, (b, hk, max_sel))
@@ -545,6 +560,7 @@ def wushkv_assign_pages(cache: WushKVCache, pool: WushKVPool, source=None, reach
     or -1 minus that where source[b] was refused."""
     torch = _torch()
     shape = (cache.batch,)
+    _check_parts(cache, pool=pool)
     for t, name in ((source, "source"), (reach, "reach")):
         if t is not None:
             _check(cache, t, name, torch.int32, shape)
@@ -569,6 +585,7 @@ def wushkv_compact_pages(cache: WushKVCache, pool: WushKVPool, bounds=None, tabl
     or, where table_out and refs_out are given, into those.  Returns (page
     table, references, n as int32 [1]), on the device."""
     torch = _torch()
+    _check_parts(cache, bounds, pool, workspace)
     handle = _launch_stream(cache, stream)
     if table_out is None:
         table_out = cache.page_table

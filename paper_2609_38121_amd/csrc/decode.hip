@@ -625,6 +625,56 @@ __device__ __forceinline__ f32x4 mfma_scaled(const i32x8 &a, const i32x8 &b, int
                                                             0, scale_b);
 }
 
+// The value codes of one word as normal fp16 numbers, 16 c: registers as
+// widen_word_f16 leaves them, all at one scale, for sums whose products lose no
+// bits to subnormal inputs.  A code masked into bits F .. of the fraction of
+// 1024 (whose bit 0 is 1) is 1024 + c 2^F, and one fused step takes it to
+// (1024 + c 2^F) 2^(4-F) - 1024 2^(4-F) = 16 c, exactly, from whatever field the
+// page has it in; only fields past the fraction are shifted first.  The
+// constants stay in registers (an instruction takes one that is not).
+template <int BITS>
+struct WidenNormal {
+    uint32_t one;       // 1024, twice
+    f16x2 add[5];       // -1024 2^(4-F), F = 0, 2, 4, 6, 8
+    __device__ __forceinline__ void init()
+    {
+        uint32_t v[6] = {0x64006400u, 0xF400F400u, 0xEC00EC00u, 0xE400E400u, 0xDC00DC00u, 0xD400D400u};
+#pragma unroll
+        for (int i = 0; i < 6; ++i) asm volatile("" : "+v"(v[i]));
+        one = v[0];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) add[i] = __builtin_bit_cast(f16x2, v[1 + i]);
+    }
+    template <int F>
+    __device__ __forceinline__ uint32_t at(uint32_t x) const
+    {
+        constexpr uint32_t code = (1u << BITS) - 1u;
+        constexpr float mul = F == 0 ? 16.0f : F == 2 ? 4.0f : F == 4 ? 1.0f : F == 6 ? 0.25f : 0.0625f;
+        const f16x2 v = __builtin_bit_cast(f16x2, (x & ((code << F) | (code << (F + 16)))) | one);
+        const f16x2 m = {(_Float16)mul, (_Float16)mul};
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, m, add[F / 2]));
+    }
+    __device__ __forceinline__ void word(uint32_t w, uint32_t *out) const
+    {
+        if constexpr (BITS == 2) {
+            const uint32_t r4 = w >> 4, r6 = w >> 6;
+            out[0] = at<6>(w);
+            out[1] = at<6>(r4);  // field 10
+            out[2] = at<8>(w);
+            out[3] = at<8>(r4);  // field 12
+            out[4] = at<2>(w);
+            out[5] = at<0>(w);
+            out[6] = at<4>(w);
+            out[7] = at<8>(r6);  // field 14
+        } else {
+            out[0] = at<4>(w);
+            out[1] = at<0>(w);
+            out[2] = at<4>(w >> 4);  // field 8
+            out[3] = at<4>(w >> 8);  // field 12
+        }
+    }
+};
+
 // LDS per wave: page stages (also the merge buffer) and the weight buffer.
 template <int D, int BITS, int G>
 struct MainLds {

@@ -11,9 +11,16 @@
 // not depend on an order of summation.  The rows of the 16x16x64 products are
 // (query head, digit) pairs, the columns pages.
 //
-// page_bounds_kernel   one wave per (page, kv head).
-// score_kernel         grid (kv heads, runs of pages, sequences).
-// select_kernel        one workgroup per (kv head, sequence).
+// page_bounds_kernel   one wave per (page, kv head).  Bound by its vector
+//                      instructions (672 a wave): 8096 page-heads at d = 128,
+//                      2-bit, 11.9 us, of which a launch is about 4.
+// select_row_kernel    rows of at most 512 planned pages: one workgroup per (kv
+//                      head, sequence), one launch.  512 rows of 380 pages 16.6
+//                      us (52 MB of boxes; 10.8 at a copy's rate): q~ in fp64
+//                      about 3, the selection about 3, the launch about 4.
+// score_kernel         longer rows: grid (kv heads, runs of pages, sequences),
+// select_kernel        then one workgroup per (kv head, sequence).  8 rows of 2046
+//                      pages 16 us, two launches' fixed cost and two latency chains.
 #include "common.h"
 #include "merge.h"
 
@@ -437,7 +444,7 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t x)
 // above it and as many equal ones as are missing.
 template <int NW>
 struct TakeLds {
-    uint32_t hist[4][256];
+    uint32_t hist[4 * 256];  // a pass each
     uint32_t range[2][NW];
     int32_t count[2][NW];
 };
@@ -466,10 +473,10 @@ __device__ __forceinline__ void take_largest(uint32_t key, int32_t page, int32_t
         for (int pass = 0; bits > 0; ++pass) {
             const int shift = max(bits - 8, 0);
             const bool in = key != 0 && (bits == 32 || (key >> bits) == (at >> bits));
-            if (in) atomicAdd(&lds.hist[pass][(key >> shift) & ((1u << (bits - shift)) - 1u)], 1u);
+            if (in) atomicAdd(&lds.hist[256 * pass + ((key >> shift) & ((1u << (bits - shift)) - 1u))], 1u);
             __syncthreads();
             // lane l: digits 252 - 4 l .. 255 - 4 l, from the top
-            const uint4 c = *reinterpret_cast<const uint4 *>(&lds.hist[pass][252 - 4 * lane]);
+            const uint4 c = *reinterpret_cast<const uint4 *>(&lds.hist[256 * pass + 252 - 4 * lane]);
             const int32_t up[4] = {(int32_t)c.w, (int32_t)c.z, (int32_t)c.y, (int32_t)c.x};
             int32_t above = wave_scan(up[0] + up[1] + up[2] + up[3]) - (up[0] + up[1] + up[2] + up[3]);
             int32_t digit = -1, rank = 0;
@@ -549,7 +556,7 @@ __global__ void __launch_bounds__(512, 4) select_row_kernel(SelectArgs a)
         finish_row<NT>(a, sp, k, row, sel, tid);
         return;
     }
-    for (int i = tid; i < 4 * 256; i += NT) take.hist[0][i] = 0;
+    for (int i = tid; i < 4 * 256; i += NT) take.hist[i] = 0;
     BoxTile<D> tile[T];
     auto load = [&](int i) __attribute__((always_inline)) {
         tile[i].load(a, h, first + 16 * i < sp.full ? phys[i] : -1, lane);

@@ -129,6 +129,13 @@ def test_bindings_check_tensors():
         lambda: wk.wushkv_sparse_attention(c, q, t, i32(2, 2), i32(2, 2)),
         lambda: wk.wushkv_sparse_attention(c, q, t, i32(2, 2, 3)[:, :, ::2], i32(2, 2)),
         lambda: wk.wushkv_sparse_attention(c, q, t, i32(2, 2, 3), i32(2)),
+        lambda: wk.wushkv_page_bounds(c, wk.WushKVBounds(full)),
+        lambda: wk.wushkv_select_pages(c, wk.WushKVBounds(full), q, t, 2),
+        lambda: wk.wushkv_select_pages(c, bounds, q, t, 2, workspace=i32(8, 8)[:, ::2]),
+        lambda: wk.wushkv_sparse_attention(c, q, t, i32(2, 2, 3), i32(2, 2), workspace=i32(8, 8)[:, ::2]),
+        lambda: wk.wushkv_assign_pages(c, counts),
+        lambda: wk.wushkv_compact_pages(c, counts),
+        lambda: wk.wushkv_compact_pages(c, pool, bounds=wk.WushKVBounds(full)),
         lambda: wk.wushkv_assign_pages(c, pool, source=i32(1)),
         lambda: wk.wushkv_assign_pages(c, pool, reach=i32(2).float()),
     ]
