@@ -19,7 +19,7 @@
 //   compact_move_kernel  the pages, the boxes, references and table entries.
 // What bounds them: small calls are launches (about 4 us each) and the one
 // workgroup's dependent reads; large ones are copies, 64 sequences with 56 forks
-// 17.3 us a call for 46 MB written (their sources are read from the caches), 1280
+// 17.3 us a call for 46 MB written (their sources are read from the caches), 1950
 // moved pages of 36 KB with their boxes 28 us, 5.3 TB/s read and written.
 #include "common.h"
 #include "merge.h"
@@ -122,8 +122,8 @@ __device__ __forceinline__ int32_t block_scan(int32_t x, int32_t *sums, int32_t 
 }
 
 // Up to 2 NT 16-byte units, by NT threads.  The stores are nontemporal: lines
-// that nothing reads soon, kept, cost the caches twice the time (111 windows and
-// 56 pages of 56 forks 29.3 us, so 14.6; 1280 moved pages 56.7, so 28.3), and two
+// that nothing reads soon, kept, cost the caches twice the time (112 windows and
+// 56 pages of 56 forks 29.3 us, so 14.6; 1950 moved pages 56.7, so 28.3), and two
 // units a thread are the best of 1 to 16 (30.3, 28.3, 38.4, 46.6, 33.2).
 template <int NT>
 __device__ __forceinline__ void copy_units(const u32x4 *src, u32x4 *dst, int64_t n)
