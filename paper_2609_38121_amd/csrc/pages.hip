@@ -19,7 +19,7 @@
 //   compact_move_kernel  the pages, the boxes, references and table entries.
 // What bounds them: small calls are launches (about 4 us each) and the one
 // workgroup's dependent reads; large ones are copies, 64 sequences with 56 forks
-// 17.3 us a call for 46 MB written (their sources are read from the caches), 1950
+// 16 us a call for 44 MB written (their sources are read from the caches), 1950
 // moved pages of 36 KB with their boxes 28 us, 5.3 TB/s read and written.
 #include "common.h"
 #include "merge.h"

@@ -797,7 +797,7 @@ extern "C" size_t wushkv_select_workspace_bytes(const wushkv_cache *c, int32_t n
 template <int D, int PASSES>
 static void launch_select(SelectArgs a, int32_t batch, hipStream_t s)
 {
-    constexpr int NT = 256;
+    constexpr int NT = 512;
     const dim3 rows((unsigned)a.n_kv, (unsigned)batch);
     // Up to 512 pages a row is one workgroup's work in one launch (8 rows of 100
     // pages 11.4 us a call, in two launches 14.6; 512 rows of 500, 21 and 28).
@@ -852,10 +852,11 @@ extern "C" int wushkv_select_pages(const wushkv_cache *c, const wushkv_bounds *b
     const int64_t pages = span > 0 ? (span + kPage - 1) / kPage : 0;
     a.planned = (int32_t)(pages < c->max_pages_per_seq ? pages : c->max_pages_per_seq);
     if (c->page_table == nullptr) a.planned = 0;
-    // two workgroups per compute unit, of 64 pages at least
+    // a workgroup of eight waves per compute unit, a tile for each wave at least
+    // (64 rows of 2000 pages 22.5 us a call; two of four waves 25)
     const int64_t rows = (int64_t)c->batch * c->n_kv_heads;
-    a.run = (int32_t)((a.planned * rows + 511) / 512 + 63) / 64 * 64;
-    if (a.run < 64) a.run = 64;
+    a.run = (int32_t)((a.planned * rows + 255) / 256 + 127) / 128 * 128;
+    if (a.run < 128) a.run = 128;
     while ((a.planned + a.run - 1) / a.run > 65535) a.run *= 2;
     a.top_k = top_k;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);

@@ -302,3 +302,38 @@ def test_pages_beyond_four_gigabytes(gpu):
     wk.wushkv_compact_pages(c, pool, bounds=b)
     assert torch.equal(c.pages.view(n, 8, -1)[:k].cpu(), torch.from_numpy(h.pages[h.used]))
     assert np.array_equal(b.codes[:k].cpu().numpy(), codes) and np.array_equal(b.scales[:, :k].cpu().numpy(), scales)
+
+
+def test_forks_and_compactions_replayed(gpu):
+    """Frees, forks, extensions and a compaction captured once and replayed with
+    other source maps, against the plain forms, value for value."""
+    rng = np.random.default_rng(51)
+    h = Host(rng, rng.integers(0, 600, 12), 2, 64, 2, spare=25, max_pages=10)
+    c, pool = h.cache(gpu)
+    source, reach = torch.zeros(12, dtype=torch.int32, device=gpu), torch.zeros(12, dtype=torch.int32, device=gpu)
+    bounds = wk.WushKVBounds(c)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        status = wk.wushkv_assign_pages(c, pool, source=source, reach=reach)
+        wk.wushkv_page_bounds(c, bounds)
+        _, _, live = wk.wushkv_compact_pages(c, pool, bounds=bounds)
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(6):
+        src = np.where(rng.random(12) < 0.5, np.arange(12), rng.integers(-1, 12, 12))
+        want = rng.integers(0, 640, 12) * (rng.random(12) < 0.3)
+        source.copy_(dev_i32(src, gpu))
+        reach.copy_(dev_i32(want, gpu))
+        if i % 2:
+            torch.cuda.synchronize()
+        graph.replay()
+        expect = pages_ref.assign(h, src, want)
+        n = pages_ref.compact(h)
+        torch.cuda.synchronize()
+        assert np.array_equal(status.cpu().numpy(), expect) and int(live[0]) == n
+        same_state(c, pool, h)
+        for b in range(h.b):
+            for lp in range(min(h.complete(b), int(h.held[b]))):
+                p = h.table[b, lp]
+                codes, scale = pages_ref.box(h.stored(p, 1))
+                assert np.array_equal(bounds.codes[p, 1].cpu().numpy(), codes) and float(bounds.scales[1, p]) == scale

@@ -186,6 +186,40 @@ def test_large_value_scales(gpu, batch, d, bits):
         assert (np.abs(got[pick] - want).max(-1) <= tol).all()
 
 
+@pytest.mark.parametrize("s_sink,win_slots,s_keep,s_flush", [(0, 64, 32, 8), (70, 128, 32, 5), (9, 256, 180, 16), (0, 64, 0, 1)])
+@pytest.mark.parametrize("batch", [5, 140])
+def test_other_windows(gpu, s_sink, win_slots, s_keep, s_flush, batch):
+    """Boxes, selection, attention and forks with no sink, one that spans tiles,
+    and long rings."""
+    rng = np.random.default_rng([s_sink, win_slots, batch])
+    lens = np.concatenate([[0, 1, s_sink, s_sink + s_keep + 1, 400], rng.integers(0, 60, batch - 5)])
+    h = Host(rng, lens, 2, 128, 2, s_sink=s_sink, s_keep=s_keep, s_flush=s_flush, win_slots=win_slots, spare=12, max_pages=8)
+    q = synth.to_bf16_bits(rng.standard_normal((batch, 4, 128)))
+    t = pages_ref.transform(rng, 2, 128)
+    c, pool = h.cache(gpu)
+    bounds = wk.WushKVBounds(c)
+    codes, scales = np.zeros((h.n_pages, 2, 2, 128), np.int8), np.zeros((2, h.n_pages), np.float32)
+    for b in range(5):
+        for lp in range(h.complete(b)):
+            for k in range(2):
+                codes[h.table[b, lp], k], scales[k, h.table[b, lp]] = pages_ref.box(h.stored(h.table[b, lp], k))
+    pick = np.arange(5)
+    for _ in range(2):  # as it is, and with the long sequence forked into two others
+        wk.wushkv_page_bounds(c, bounds)
+        sel, n = wk.wushkv_select_pages(c, bounds, bf16(q, gpu), torch.from_numpy(t).to(gpu), 3)
+        few = some(h, pick)
+        rsel, rn = pages_ref.select(few, pages_ref.scores(few, codes, scales, q[pick], t), 3)
+        sel, n = sel.cpu().numpy(), n.cpu().numpy()
+        assert np.array_equal(sel[pick], rsel) and np.array_equal(n[pick], rn)
+        got = run(gpu, h, q, t, sel, n, cache=c)
+        want, tol = pages_ref.attention(few, q[pick], t, sel[pick], n[pick], 1.0 / np.sqrt(128))
+        assert (np.abs(got[pick] - want).max(-1) <= tol).all()
+        source = np.arange(batch)
+        source[[0, 2]] = 4
+        status = wk.wushkv_assign_pages(c, pool, source=dev_i32(source, gpu))
+        assert np.array_equal(status.cpu().numpy(), pages_ref.assign(h, source))
+
+
 # ------------------------------------------------------------------ together
 
 
