@@ -202,6 +202,7 @@ class WushKVBounds:
         self.codes = torch.zeros(cache.n_pages, cache.n_kv_heads, 2, cache.head_dim, dtype=torch.int8,
                                  device=cache.device)
         self.scales = torch.zeros(cache.n_kv_heads, cache.n_pages, dtype=torch.float32, device=cache.device)
+        self._of = (cache.n_pages, cache.n_kv_heads, cache.head_dim, self.codes.get_device())
         self._desc = BoundsDesc(self.codes.data_ptr(), self.scales.data_ptr())
 
     @property
@@ -221,6 +222,7 @@ class WushKVPool:
         pages = cache.page_table[there].long()
         self.refs = torch.bincount(pages, minlength=cache.n_pages).to(torch.int32)
         self.low = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        self._of = (cache.n_pages, cache.batch, self.refs.get_device())
         self._desc = PoolDesc(self.refs.data_ptr(), self.held.data_ptr(), self.low.data_ptr())
 
     @property
@@ -417,32 +419,41 @@ def wushkv_dequant(cache: WushKVCache, b: int, start: int, count: int, k_out=Non
     return k_out, v_out
 
 
-def _check(cache, t, name, dtype, shape):
-    """A contiguous tensor of this type and shape on the cache's device."""
+def _check(dev, t, name, dtype, shape):
+    """A contiguous tensor of this type and shape on device dev."""
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, list(shape)))
-    if t.get_device() != cache.pages.get_device():
+    if t.get_device() != dev:
         raise ValueError("%s is not on the cache's device" % name)
+    return t.data_ptr()
 
 
-def _check_parts(cache, bounds=None, pool=None, workspace=None):
-    """Boxes and a pool of this cache's sizes, a workspace on its device."""
-    if bounds is not None and (bounds.codes.shape != (cache.n_pages, cache.n_kv_heads, 2, cache.head_dim)
-                               or bounds.codes.get_device() != cache.pages.get_device()):
-        raise ValueError("bounds are not this cache's")
-    if pool is not None and (pool.refs.numel() != cache.n_pages or pool.held.numel() != cache.batch
-                             or pool.refs.get_device() != cache.pages.get_device()):
-        raise ValueError("pool is not this cache's")
-    if workspace is not None and (not workspace.is_contiguous() or workspace.get_device() != cache.pages.get_device()):
+def _check_space(dev, t):
+    if not t.is_contiguous() or t.get_device() != dev:
         raise ValueError("workspace must be contiguous and on the cache's device")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _launch_stream(cache, stream):
-    """The stream handle of a call on the cache's device, which has to be the
-    current one."""
+def _bounds_of(cache, dev, bounds):
+    """Boxes of this cache's sizes, on its device."""
+    if bounds._of != (cache.n_pages, cache.n_kv_heads, cache.head_dim, dev):
+        raise ValueError("bounds are not this cache's")
+    return ctypes.byref(bounds._desc)
+
+
+def _pool_of(cache, dev, pool):
+    """A pool of this cache's sizes, on its device."""
+    if pool._of != (cache.n_pages, cache.batch, dev):
+        raise ValueError("pool is not this cache's")
+    return ctypes.byref(pool._desc)
+
+
+def _launch_stream(dev, stream):
+    """The stream handle of a call on device dev, which has to be the current
+    one."""
     torch = _torch()
     current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)()
-    if cache.pages.get_device() != current:
+    if dev != current:
         raise ValueError("the cache's device is not the current one")
     if stream is not None:
         if stream.device_index != current:
@@ -464,13 +475,12 @@ def wushkv_page_bounds(cache: WushKVCache, bounds: WushKVBounds, since=None, max
     """The boxes of the pages completed since quant_end was ``since`` (int32
     [batch] on the device; None: of all complete pages), at most ``max_new``
     (by default max_pages) a sequence."""
-    torch = _torch()
-    _check_parts(cache, bounds)
-    if since is not None:
-        _check(cache, since, "since", torch.int32, (cache.batch,))
+    dev = cache.pages.get_device()
+    box = _bounds_of(cache, dev, bounds)
+    at = None if since is None else _check(dev, since, "since", _torch().int32, (cache.batch,))
     st = _lib.lib().wushkv_page_bounds(
-        ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(since),
-        cache.max_pages if max_new is None else operator.index(max_new), _launch_stream(cache, stream))
+        ctypes.byref(cache._desc), box, at, cache.max_pages if max_new is None else operator.index(max_new),
+        _launch_stream(dev, stream))
     check(st, "wushkv_page_bounds")
 
 
@@ -487,32 +497,31 @@ def wushkv_select_pages(cache: WushKVCache, bounds: WushKVBounds, q, t_k_inv, to
     [batch][n_kv]); ``scores``, if given, fp32 [batch][n_kv][max_pages],
     receives every complete page's score."""
     torch = _torch()
+    dev = cache.pages.get_device()
     b, hk, d, top_k = cache.batch, cache.n_kv_heads, cache.head_dim, operator.index(top_k)
     n_q = q.shape[1] if q.dim() == 3 else 0
-    _check_parts(cache, bounds, workspace=workspace)
-    _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
-    _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
-    if scores is not None:
-        _check(cache, scores, "scores", torch.float32, (b, hk, cache.max_pages))
-    if max_seq_len is None:
-        max_seq_len = cache.max_seq_len
-    max_seq_len = operator.index(max_seq_len)
-    handle = _launch_stream(cache, stream)
+    box = _bounds_of(cache, dev, bounds)
+    q_at = _check(dev, q, "q", torch.bfloat16, (b, n_q, d))
+    t_at = _check(dev, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    scores_at = None if scores is None else _check(dev, scores, "scores", torch.float32, (b, hk, cache.max_pages))
+    max_seq_len = cache.max_seq_len if max_seq_len is None else operator.index(max_seq_len)
+    if workspace is not None:
+        space = _check_space(dev, workspace)
+    handle = _launch_stream(dev, stream)
     if workspace is None:
         need = wushkv_select_workspace_bytes(cache, n_q, max_seq_len, top_k)
         if need == 0:
             raise WushKVError(_lib.EINVAL, "wushkv_select_workspace_bytes")
         workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+        space = workspace.data_ptr(), need
     shape = (b, hk, top_k + 1)
     if sel is None:
         sel = _on_stream(torch.empty(shape, dtype=torch.int32, device=q.device), stream)
     if n_sel is None:
         n_sel = _on_stream(torch.empty(b, hk, dtype=torch.int32, device=q.device), stream)
-    _check(cache, sel, "sel", torch.int32, shape)
-    _check(cache, n_sel, "n_sel", torch.int32, (b, hk))
     st = _lib.lib().wushkv_select_pages(
-        ctypes.byref(cache.desc), ctypes.byref(bounds.desc), _ptr(q), n_q, max_seq_len, _ptr(t_k_inv), top_k,
-        _ptr(sel), _ptr(n_sel), _ptr(scores), _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
+        ctypes.byref(cache._desc), box, q_at, n_q, max_seq_len, t_at, top_k, _check(dev, sel, "sel", torch.int32, shape),
+        _check(dev, n_sel, "n_sel", torch.int32, (b, hk)), scores_at, space[0], space[1], handle)
     check(st, "wushkv_select_pages")
     return sel, n_sel
 
@@ -527,27 +536,29 @@ def wushkv_sparse_attention(cache: WushKVCache, q, t_k_inv, sel, n_sel, sm_scale
     pages: sel int32 [batch][n_kv][max_sel] logical pages, of which the first
     n_sel (int32 [batch][n_kv]) count.  Returns fp32 [batch][n_q][d]."""
     torch = _torch()
+    dev = cache.pages.get_device()
     b, hk, d = cache.batch, cache.n_kv_heads, cache.head_dim
     n_q = q.shape[1] if q.dim() == 3 else 0
     max_sel = sel.shape[2] if sel.dim() == 3 else 0
-    _check_parts(cache, workspace=workspace)
-    _check(cache, q, "q", torch.bfloat16, (b, n_q, d))
-    _check(cache, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
-    _check(cache, sel, "sel", torch.int32, (b, hk, max_sel))
-    _check(cache, n_sel, "n_sel", torch.int32, (b, hk))
+    q_at = _check(dev, q, "q", torch.bfloat16, (b, n_q, d))
+    t_at = _check(dev, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    sel_at = _check(dev, sel, "sel", torch.int32, (b, hk, max_sel))
+    n_at = _check(dev, n_sel, "n_sel", torch.int32, (b, hk))
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
-    handle = _launch_stream(cache, stream)
+    if workspace is not None:
+        space = _check_space(dev, workspace)
+    handle = _launch_stream(dev, stream)
     if out is None:
         out = _on_stream(torch.empty(b, n_q, d, dtype=torch.float32, device=q.device), stream)
-    _check(cache, out, "out", torch.float32, (b, n_q, d))
     if workspace is None:
         # (sizes without a plan: the call says what is wrong)
         need = max(16, wushkv_sparse_workspace_bytes(cache, n_q, max_sel))
         workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+        space = workspace.data_ptr(), need
     st = _lib.lib().wushkv_sparse_attention(
-        ctypes.byref(cache.desc), _ptr(q), n_q, _ptr(sel), _ptr(n_sel), max_sel, _ptr(t_k_inv), float(sm_scale),
-        _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
+        ctypes.byref(cache._desc), q_at, n_q, sel_at, n_at, max_sel, t_at, float(sm_scale),
+        _check(dev, out, "out", torch.float32, (b, n_q, d)), space[0], space[1], handle)
     check(st, "wushkv_sparse_attention")
     return out
 
@@ -559,17 +570,15 @@ def wushkv_assign_pages(cache: WushKVCache, pool: WushKVPool, source=None, reach
     int32 [batch] on the device.  Returns status int32 [batch]: pages missing,
     or -1 minus that where source[b] was refused."""
     torch = _torch()
-    shape = (cache.batch,)
-    _check_parts(cache, pool=pool)
-    for t, name in ((source, "source"), (reach, "reach")):
-        if t is not None:
-            _check(cache, t, name, torch.int32, shape)
-    handle = _launch_stream(cache, stream)
+    dev, shape = cache.pages.get_device(), (cache.batch,)
+    books = _pool_of(cache, dev, pool)
+    source_at = None if source is None else _check(dev, source, "source", torch.int32, shape)
+    reach_at = None if reach is None else _check(dev, reach, "reach", torch.int32, shape)
+    handle = _launch_stream(dev, stream)
     if status is None:
         status = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
-    _check(cache, status, "status", torch.int32, shape)
-    st = _lib.lib().wushkv_assign_pages(ctypes.byref(cache.desc), ctypes.byref(pool.desc), _ptr(source), _ptr(reach),
-                                        _ptr(status), handle)
+    st = _lib.lib().wushkv_assign_pages(ctypes.byref(cache._desc), books, source_at, reach_at,
+                                        _check(dev, status, "status", torch.int32, shape), handle)
     check(st, "wushkv_assign_pages")
     return status
 
@@ -585,24 +594,27 @@ def wushkv_compact_pages(cache: WushKVCache, pool: WushKVPool, bounds=None, tabl
     or, where table_out and refs_out are given, into those.  Returns (page
     table, references, n as int32 [1]), on the device."""
     torch = _torch()
-    _check_parts(cache, bounds, pool, workspace)
-    handle = _launch_stream(cache, stream)
+    dev = cache.pages.get_device()
+    books = _pool_of(cache, dev, pool)
+    box = None if bounds is None else _bounds_of(cache, dev, bounds)
+    if workspace is not None:
+        space = _check_space(dev, workspace)
+    handle = _launch_stream(dev, stream)
     if table_out is None:
         table_out = cache.page_table
     if refs_out is None:
         refs_out = pool.refs
     if live_out is None:
         live_out = _on_stream(torch.empty(1, dtype=torch.int32, device=cache.device), stream)
-    _check(cache, table_out, "table_out", torch.int32, (cache.batch, cache.max_pages))
-    _check(cache, refs_out, "refs_out", torch.int32, (cache.n_pages,))
-    _check(cache, live_out, "live_out", torch.int32, (1,))
     if workspace is None:
         need = max(16, wushkv_compact_workspace_bytes(cache))
         workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=cache.device), stream)
+        space = workspace.data_ptr(), need
     st = _lib.lib().wushkv_compact_pages(
-        ctypes.byref(cache.desc), ctypes.byref(pool.desc), None if bounds is None else ctypes.byref(bounds.desc),
-        _ptr(table_out), _ptr(refs_out), _ptr(live_out), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), handle)
+        ctypes.byref(cache._desc), books, box,
+        _check(dev, table_out, "table_out", torch.int32, (cache.batch, cache.max_pages)),
+        _check(dev, refs_out, "refs_out", torch.int32, (cache.n_pages,)),
+        _check(dev, live_out, "live_out", torch.int32, (1,)), space[0], space[1], handle)
     check(st, "wushkv_compact_pages")
     return table_out, refs_out, live_out
 
