@@ -311,7 +311,8 @@ __global__ void __launch_bounds__(kBlock / 4) compact_count_kernel(CompactArgs a
 }
 
 // COUNTED: the blocks' counts are there; otherwise every workgroup counts the
-// (few) blocks itself.
+// (few) blocks itself.  Workgroups start in any order, and each reads references
+// of other blocks: in place, this launch therefore writes none of them.
 template <bool COUNTED>
 __global__ void __launch_bounds__(kBlock / 4) compact_plan_kernel(CompactArgs a)
 {
@@ -335,7 +336,6 @@ __global__ void __launch_bounds__(kBlock / 4) compact_plan_kernel(CompactArgs a)
     }
     const int32_t live = block_sum(all, sums);
     before = block_sum(before, sums);
-    // (references below n keep their values in this launch, also in place)
     int32_t below = 0;
     const int32_t whole = live / kBlock;
     if constexpr (COUNTED) {
@@ -358,15 +358,14 @@ __global__ void __launch_bounds__(kBlock / 4) compact_plan_kernel(CompactArgs a)
         const int64_t p = p0 + e;
         if (p >= a.n_pages) break;
         if (p < live) {
-            if (v[e] > 0) a.refs_out[p] = v[e];
-            else a.hole[p - at] = (int32_t)p;
+            if (v[e] <= 0) a.hole[p - at] = (int32_t)p;
+            else if (a.refs_out != a.refs) a.refs_out[p] = v[e];
         } else {
             if (v[e] > 0) {
                 a.mover[at - below] = (int32_t)p;
                 a.mover_refs[at - below] = v[e];
             }
             a.rank[p] = v[e] > 0 ? at - below : -1;
-            a.refs_out[p] = 0;
         }
         at += v[e] > 0;
     }
@@ -376,6 +375,8 @@ __global__ void __launch_bounds__(256) compact_move_kernel(CompactArgs a)
 {
     const int tid = threadIdx.x;
     const int32_t live = a.head[0], moves = a.head[1];
+    // (the moves write references below n only)
+    for (int64_t p = (int64_t)live + blockIdx.x * 256 + tid; p < a.n_pages; p += (int64_t)gridDim.x * 256) a.refs_out[p] = 0;
     if ((int32_t)blockIdx.x < a.table_blocks) {
         const int64_t n = (int64_t)a.batch * a.max_pages;
         for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < n; i += (int64_t)a.table_blocks * 256) {
