@@ -538,8 +538,14 @@ typedef struct wushkv_pool {
  *           reach too.
  *   status  int32 [batch]: the number of pages missing because the pool ran
  *           out (their entries are -1 and held ends before them), or, where
- *           source[b] was refused, -1 minus that number.  A fork whose own page
- *           is missing lacks the positions in it.
+ *           source[b] was refused, -1 minus that number.
+ *
+ * A fork whose own page is missing lacks the positions in it (64 held[b] falls
+ * short of min(quant_end[b], seq_len[b]) - s_sink): attention leaves them out.
+ * Nothing fills a page that it gets for them afterwards.  The caller therefore
+ * frees it, or makes it a copy of a sequence that has all of its pages, before
+ * it is given pages (reach), appended to or forked; otherwise what such a page
+ * held before is attended to.
  *
  * Pages are handed out in the order of the sequences and, for each, of its
  * logical pages, the lowest free one first: the result depends on nothing else.

@@ -568,7 +568,9 @@ def wushkv_assign_pages(cache: WushKVCache, pool: WushKVPool, source=None, reach
     frees it, s makes it a copy of the kept sequence s (None keeps all);
     reach[b]: positions it is to hold pages for (None: no new ones).  Both
     int32 [batch] on the device.  Returns status int32 [batch]: pages missing,
-    or -1 minus that where source[b] was refused."""
+    or -1 minus that where source[b] was refused.  A copy whose page being
+    filled is missing (64 held < quantised positions) is freed, or copied from a
+    whole sequence again, before it is given pages, appended to or forked."""
     torch = _torch()
     dev, shape = cache.pages.get_device(), (cache.batch,)
     books = _pool_of(cache, dev, pool)

@@ -256,7 +256,8 @@ __global__ void __launch_bounds__(256) assign_copy_kernel(AssignArgs a)
     if (source_kind(a, b, s) != kFork) return;
     const int64_t at = (int64_t)(blockIdx.x % a.copy_blocks) * kCopyUnits;
     const int32_t q = quantised(a, s), lp = q / kPage;
-    if (q % kPage == 0 || lp >= a.max_pages || lp >= a.held[b]) return;
+    // (neither row is read beyond what its sequence holds)
+    if (q % kPage == 0 || lp >= a.max_pages || lp >= a.held[b] || lp >= a.held[s]) return;
     const int32_t from = a.page_table[(int64_t)s * a.max_pages + lp], to = a.page_table[(int64_t)b * a.max_pages + lp];
     if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) return;
     u32x4 *pool = reinterpret_cast<u32x4 *>(a.pages);

@@ -89,3 +89,22 @@ def test_assignments_and_compactions_in_any_order(L, seed):
                 assert np.array_equal(s.assign(L, source, reach), want), (step, order)
         for order, s in zip(ORDERS, states):
             assert same(s, h), (step, order)
+
+
+def test_a_fork_copies_no_page_that_its_source_does_not_hold(L):
+    """A row is valid up to held: an entry behind it, here another sequence's page,
+    is not what a fork's own page is filled from."""
+    h = Host(np.random.default_rng(9), [500, 333, 0], 1, 64, 2, spare=4)
+    full = h.complete(0)
+    assert h.every(0) == full + 1 == h.held[0]
+    h.refs[h.table[0, full]] -= 1  # sequence 0 never got the page it was filling ..
+    h.held[0] = full
+    h.table[0, full] = h.table[1, 0]  # .. and its row names something old there
+    for entries in (0, 300):  # (with many entries the rows have a launch of their own)
+        big = copy.deepcopy(h)
+        big.max_pages += entries
+        big.table = np.pad(big.table, ((0, 0), (0, entries)), constant_values=-1)
+        s = State(big)
+        status = s.assign(L, [0, 1, 0])
+        assert status.tolist() == [0, 0, 0] and s.held.tolist() == [full, h.held[1], full + 1]
+        assert np.array_equal(s.pages, h.pages)
