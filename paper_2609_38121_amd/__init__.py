@@ -100,7 +100,26 @@ def wushkv_timing_launches():
     return out
 
 
-class WushKVCache:
+class _Described:
+    """Device arrays and the C descriptor that names them.  A program may put
+    another contiguous tensor of the same type, shape and device in an array's
+    place: the descriptor follows it (a captured graph keeps the old one)."""
+
+    def __setattr__(self, name, value):
+        desc = self.__dict__.get("_desc")
+        if desc is not None and name in _FIELDS[type(desc)]:
+            old = self.__dict__[name]
+            if not isinstance(value, _torch().Tensor) or value.device != old.device:
+                raise ValueError("%s must be a tensor on %s" % (name, old.device))
+            setattr(desc, name, _check(old.get_device(), value, name, old.dtype, old.shape))
+        object.__setattr__(self, name, value)
+
+
+# the arrays of each descriptor
+_FIELDS = {d: frozenset(n for n, t in d._fields_ if t is ctypes.c_void_p) for d in (CacheDesc, BoundsDesc, PoolDesc)}
+
+
+class WushKVCache(_Described):
     """Device memory of one WUSH-KV cache plus its C descriptor.
 
     Allocates (torch, on ``device``): the page pool, the page table, the bf16
@@ -192,7 +211,7 @@ class WushKVCache:
         return new
 
 
-class WushKVBounds:
+class WushKVBounds(_Described):
     """The boxes of a cache's complete pages (wushkv_page_bounds): ``codes``
     int8 [n_pages][n_kv][2][d], centres then radii, and ``scales`` fp32
     [n_kv][n_pages], zero-initialised on the cache's device."""
@@ -210,7 +229,7 @@ class WushKVBounds:
         return self._desc
 
 
-class WushKVPool:
+class WushKVPool(_Described):
     """The bookkeeping of a cache's pages (wushkv_assign_pages): ``refs`` int32
     [n_pages], ``held`` int32 [batch] and ``low`` int32 [1].  Starts from the
     cache's page table: every entry of it is one reference."""
@@ -593,8 +612,9 @@ def wushkv_compact_pages(cache: WushKVCache, pool: WushKVPool, bounds=None, tabl
                          live_out=None, workspace=None, stream=None):
     """Moves the n pages in use to the physical pages 0 .. n - 1 (with their
     boxes, if bounds is given).  The page table and references change in place
-    or, where table_out and refs_out are given, into those.  Returns (page
-    table, references, n as int32 [1]), on the device."""
+    or, where table_out and refs_out are given, into those, which the caller
+    then swaps in (cache.page_table, pool.refs = table_out, refs_out) or copies
+    over.  Returns (page table, references, n as int32 [1]), on the device."""
     torch = _torch()
     dev = cache.pages.get_device()
     books = _pool_of(cache, dev, pool)

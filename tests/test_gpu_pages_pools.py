@@ -51,3 +51,26 @@ def test_compaction_of_large_pools(gpu, n_pages, share):
         assert np.array_equal(bounds.codes.cpu().numpy(), wcodes) and np.array_equal(bounds.scales.cpu().numpy(), wscales)
         if not in_place:
             assert np.array_equal(c.page_table.cpu().numpy(), h.table) and np.array_equal(pool.refs.cpu().numpy(), h.refs)
+
+
+def test_arrays_of_a_compaction_swapped_in(gpu):
+    """The new table and references put in the old ones' place, twice in turn, with
+    calls on them in between."""
+    rng = np.random.default_rng(11)
+    h = pages_ref.Host(rng, [600, 333, 0, 90], 2, 64, 2, spare=9, max_pages=12)
+    c, pool = h.cache(gpu)
+    for step in range(3):
+        old = c.page_table, pool.refs
+        source = np.arange(4)
+        source[step % 2] = -1 if step < 2 else 3
+        status = wk.wushkv_assign_pages(c, pool, source=torch.tensor(source, dtype=torch.int32, device=gpu))
+        assert np.array_equal(status.cpu().numpy(), pages_ref.assign(h, source))
+        table, refs, _ = wk.wushkv_compact_pages(c, pool, table_out=torch.empty_like(c.page_table),
+                                                 refs_out=torch.empty_like(pool.refs))
+        c.page_table, pool.refs = table, refs
+        pages_ref.compact(h)
+        for t in old:
+            t.fill_(-77)
+        torch.cuda.synchronize()
+        assert np.array_equal(c.page_table.cpu().numpy(), h.table) and np.array_equal(pool.refs.cpu().numpy(), h.refs)
+        assert np.array_equal(pool.held.cpu().numpy(), h.held) and np.array_equal(c.pages.cpu().numpy(), h.pages.reshape(-1))
