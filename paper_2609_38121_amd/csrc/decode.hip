@@ -2685,16 +2685,25 @@ static int check_chunk(const wushkv_cache *c, int32_t max_tok)
 // Lists: whether one workgroup takes a row's whole list and its windows.  With
 // a row for every compute unit the rows fill the device by themselves, and the
 // launch of q~, the partials and their merge fall away (d = 128, four heads,
-// 2-bit, 512 rows of 5, 33 and 65 pages: 19.8, 34.9 and 51.0 us a call instead of
-// 33.5, 47.1 and 60.9; eight heads, 4-bit, 256 rows of 129: 76 and 83).  With
-// fewer rows compute units would stand idle (128 rows of 65: 29 us, split 22; 64
-// rows of 129, 44 and 20).  A list of at most 8 pages of d = 64 is a chain of two
-// pages a wave, shorter than the second launch (9.3 us, split 11.2).  A wave's
-// pages are numbered by its lanes.
+// 2-bit, 512 rows of 1, 33 and 65 pages: 19.2, 32.1 and 46.7 us a call instead of
+// 33.6, 43.1 and 61.3; with windows of 4096 slots, 241, 253 and 266 instead of 418,
+// 423 and 372; eight heads, 4-bit, 256 rows of 65: 45 and 58).  With fewer rows
+// compute units would stand idle (64 rows of 16 pages 16.4 us, split 12.3; 8 rows of
+// 65, 28.6 and 10.4).
+// At d = 64 a list of at most 8 pages with at most three units of windows is a
+// chain of two pages and three tiles a wave, and one launch is less work for the
+// host than two: one row's calls one after the other 7.6, 8.1 and 8.7 us with windows
+// of 64, 128 and 192 slots and one page, split 10.4; 8.3, 8.9 and 9.5 with eight
+// pages, split 10.3 (eight heads, 4-bit: 10.8, 11.3 and 11.9, and 11.7).  Replayed from a
+// graph it is 7.2, 7.9 and 8.6 and 7.4.  Nine pages are a third for some waves, and
+// the windows of one row go to one workgroup only: 512 slots 11.8, split 10.4, 4096
+// slots 47.9, split 7.9.
+// A wave's pages are numbered by its lanes.
 static bool whole_rows(const wushkv_cache *c, int32_t max_sel)
 {
     if (max_sel > 4 * kMaxRunPages) return false;
-    return (int64_t)c->batch * c->n_kv_heads >= device_cus() || (c->head_dim == 64 && max_sel <= 8);
+    return (int64_t)c->batch * c->n_kv_heads >= device_cus() ||
+           (c->head_dim == 64 && max_sel <= 8 && c->win_slots <= 3 * kPage);
 }
 
 static size_t plan_bytes(const DecodePlan &p)
