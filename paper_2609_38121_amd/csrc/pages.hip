@@ -29,8 +29,9 @@ namespace wushkv {
 constexpr int kMaxAssignBatch = 16384;  // the sequences' starts and bases stay in LDS
 constexpr int kAssignThreads = 1024;
 constexpr int kFewSequences = 1024;     // the same, in less LDS
-// Table entries up to which the one workgroup goes through them itself: 248
-// entries 12.8 us a call, with a launch for them 14.8; 8064, 48.8 and 26.2.
+// Table entries up to which the one workgroup goes through them itself (slots
+// taken again, replayed from a graph): 248 entries 9.2 us a call, with a launch for
+// them 10.1; 1024, 10.9 and 11.1; 1536, 13.3 and 11.4; 8064, 41.8 and 16.6.
 constexpr int kOneAssign = 1024;
 
 struct AssignArgs {
@@ -267,7 +268,10 @@ __global__ void __launch_bounds__(256) assign_copy_kernel(AssignArgs a)
 // ------------------------------------------------------------------ compact
 
 constexpr int kBlock = 4096;  // references per workgroup of the count and the plan
-constexpr int kOwnCount = 8;  // blocks up to which the plan counts them itself
+// Blocks up to which the plan counts them itself (a pool with nothing to move,
+// replayed from a graph): 2 blocks 7.6 us a call, with a launch for them 8.8; 4, 8.8
+// both; 6, 10.1 and 8.9; 8, 11.4 and 8.9.
+constexpr int kOwnCount = 4;
 
 struct CompactArgs {
     uint8_t *pages;
