@@ -448,7 +448,7 @@ int wushkv_page_bounds(const wushkv_cache *c, const wushkv_bounds *bounds, const
  *
  *   q, n_q_heads, t_k_inv  as wushkv_decode_attention takes them.
  *   max_seq_len  (host) >= every seq_len[b] (pages beyond it are left out);
- *            sizes the grid and the workspace.
+ *            sizes the grid.
  *   top_k    (host) >= 0: complete pages selected per (sequence, kv head).
  *   sel      int32 [batch][n_kv_heads][top_k + 1]: logical pages, ascending;
  *            -1 from n_sel on.
@@ -474,7 +474,8 @@ int wushkv_select_pages(const wushkv_cache *c, const wushkv_bounds *bounds, cons
                         int32_t top_k, int32_t *sel, int32_t *n_sel, float *scores,
                         void *workspace, size_t workspace_bytes, wushkv_stream_t stream);
 
-/* Workspace of wushkv_select_pages, or 0 for invalid arguments. */
+/* Workspace of wushkv_select_pages (the same for every max_seq_len and top_k),
+   or 0 for invalid arguments. */
 size_t wushkv_select_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads,
                                      int32_t max_seq_len, int32_t top_k);
 
@@ -506,7 +507,8 @@ size_t wushkv_sparse_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads, i
  * A pool's bookkeeping, for caches whose sequences share one pool of pages.
  *   refs   int32 [n_pages]: page-table rows that hold the page; 0: free.  A page
  *          the caller adds a reference to is not handed out or freed (a
- *          compaction moves it like any other).
+ *          compaction moves it like any other, and names it in no table: its place
+ *          follows from the references before the call, by the rule there).
  *   held   int32 [batch]: pages sequence b holds: its page-table row is valid in
  *          [0, held[b]) and not read beyond.
  *   low    int32 [1]: no page below low[0] is free (0 is always right; kept so
@@ -573,6 +575,7 @@ int wushkv_assign_pages(const wushkv_cache *c, const wushkv_pool *pool, const in
  *              them may still run until the caller swaps them in.
  *   live_out   nullable int32 [1]: n.
  *   workspace  wushkv_compact_workspace_bytes() bytes, not initialised.
+ * table_out and refs_out otherwise overlap none of the call's arrays.
  * pool->low stays right in both cases.
  */
 int wushkv_compact_pages(const wushkv_cache *c, const wushkv_pool *pool,

@@ -18,7 +18,7 @@ def build(folder):
     for path in (os.path.join(HERE, "common.h"), os.path.join(HERE, "merge.h"), os.path.join(CSRC, "pages.hip")):
         shutil.copy(path, folder)
     so = os.path.join(folder, "libpages_host.so")
-    compiler = os.path.join(os.path.dirname(os.path.realpath(HIPCC)), "amdclang++")
+    compiler = os.path.join(os.path.dirname(os.path.realpath(shutil.which(HIPCC))), "amdclang++")
     subprocess.run([compiler, "-O2", "-std=c++17", "-fPIC", "-shared", "-x", "c++", "-I", INCLUDE,
                     os.path.join(folder, "pages.hip"), "-o", so], check=True)
     L = ctypes.CDLL(so)

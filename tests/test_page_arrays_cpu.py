@@ -38,3 +38,9 @@ def test_clones_have_arrays_of_their_own():
     d = c.clone()
     d.page_table = torch.zeros_like(d.page_table)
     assert d.desc.page_table == d.page_table.data_ptr() != c.desc.page_table == c.page_table.data_ptr()
+
+
+def test_a_selection_workspace_serves_every_length_and_count():
+    c, _, _ = make()
+    sizes = {wk.wushkv_select_workspace_bytes(c, 4, n, k) for n in (0, 100, 200, 1 << 30) for k in (0, 3, 1000)}
+    assert len(sizes) == 1 and sizes.pop() >= 4 * c.batch * c.n_kv_heads * c.max_pages
