@@ -358,19 +358,21 @@ __global__ void __launch_bounds__(kBlock / 4) compact_plan_kernel(CompactArgs a)
     int32_t sum;
     int32_t at = before + block_scan(in_use(r), sums, sum);  // pages in use before p
     const int32_t v[4] = {r.x, r.y, r.z, r.w};
+    const bool in_place = a.refs_out == a.refs;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int64_t p = p0 + e;
         if (p >= a.n_pages) break;
         if (p < live) {
             if (v[e] <= 0) a.hole[p - at] = (int32_t)p;
-            else if (a.refs_out != a.refs) a.refs_out[p] = v[e];
+            else if (!in_place) a.refs_out[p] = v[e];
         } else {
             if (v[e] > 0) {
                 a.mover[at - below] = (int32_t)p;
                 a.mover_refs[at - below] = v[e];
             }
             a.rank[p] = v[e] > 0 ? at - below : -1;
+            if (!in_place) a.refs_out[p] = 0;
         }
         at += v[e] > 0;
     }
@@ -380,8 +382,9 @@ __global__ void __launch_bounds__(256) compact_move_kernel(CompactArgs a)
 {
     const int tid = threadIdx.x;
     const int32_t live = a.head[0], moves = a.head[1];
-    // (the moves write references below n only)
-    for (int64_t p = (int64_t)live + blockIdx.x * 256 + tid; p < a.n_pages; p += (int64_t)gridDim.x * 256) a.refs_out[p] = 0;
+    // (the plan wrote no reference; the moves write those below n only)
+    if (a.refs_out == a.refs)
+        for (int64_t p = (int64_t)live + blockIdx.x * 256 + tid; p < a.n_pages; p += (int64_t)gridDim.x * 256) a.refs_out[p] = 0;
     if ((int32_t)blockIdx.x < a.table_blocks) {
         const int64_t n = (int64_t)a.batch * a.max_pages;
         for (int64_t i = (int64_t)blockIdx.x * 256 + tid; i < n; i += (int64_t)a.table_blocks * 256) {
