@@ -1361,6 +1361,14 @@ decode_main_kernel(DecodeArgs a)
             // to those of the pages' sums (through the weight buffer, 64 channels
             // at a time); one lane of a row carries l
             float *tb = reinterpret_cast<float *>(tbuf);
+            // (values of 2^112 and more leave no room for 2^lift / kOutScale: the
+            // reference then lies above the maximum, so that the factor is 1)
+            float top = 0.0f;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, fabsf(win_acc[nt][r]));
+            if (__any(top >= 0x1p112f)) lift = -4.0f;
             const float up = ldexpf(1.0f, (int)lift);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {

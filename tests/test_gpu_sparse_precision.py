@@ -84,3 +84,33 @@ def test_other_windows(gpu, s_sink, win_slots, s_keep, s_flush, batch, d):
     q = synth.to_bf16_bits(rng.standard_normal((batch, 8, d)))
     t = transform(rng, 2, d)
     close(gpu, h, q, t, *sparse_exact.lists(rng, h, 5, least=2), pick=np.arange(min(batch, 3)), what="%d slots" % win_slots)
+
+
+@pytest.mark.parametrize("d,bits,G", [(128, 2, 4), (128, 4, 8), (64, 2, 1)])
+@pytest.mark.parametrize("batch", [3, 140])
+def test_the_largest_values_in_a_window(gpu, d, bits, G, batch):
+    """Finite results of values up to bf16's largest, and the other channels' as
+    near as ever: the windows' sums have no room for a factor."""
+    rng = np.random.default_rng([d, bits, G, batch, 4])
+    h = Host(rng, [333, 90, 20] + [40] * (batch - 3), 2, d, bits)
+    q = synth.to_bf16_bits(rng.standard_normal((batch, 2 * G, d)) * 0.3)
+    t = transform(rng, 2, d)
+    last = [p if p < 4 else 4 + (p - 4) % 60 for p in h.seq_len - 1]
+    big = np.float32([3.3e38, -1e36, 5e34])
+    for b in range(3):
+        h.win_v[b, :, 5, last[b]] = synth.to_bf16_bits(big[b:b + 1])[0]
+    sel, n = sparse_exact.lists(rng, h, 4, least=2)
+    got = run(gpu, h, q, t, sel, n)[:3]
+    finite = bool(np.isfinite(got).all())
+    assert finite
+    few = some(h, np.arange(3))
+    want, _ = sparse_exact.rows(few, q[:3], t, sel[:3], n[:3])
+    assert (np.abs(got[..., 5] - want[..., 5]) <= 4e-6 * np.abs(want[..., 5])).all()
+    # the other channels: as if that one value were not there
+    few.win_v = few.win_v.copy()
+    few.win_v[:, :, 5] = 0
+    want, tol = sparse_exact.rows(few, q[:3], t, sel[:3], n[:3])
+    got[..., 5] = want[..., 5]
+    # (weights of 2^-4 at most leave fp16 parts of 2^-21 of the largest, not 2^-33)
+    room = 2.0 ** -21 * 15.0 * 2.0 * np.sqrt(64.0 * 4 * d)
+    assert (np.linalg.norm(got - want, axis=-1) <= 3.0 * tol[0] + tol[1] + room).all()
