@@ -26,6 +26,14 @@
  *   wushkv_assign_pages, wushkv_compact_pages
  *                            sequences freed, forked and given pages; the
  *                            pages in use moved to the front of the pool
+ *   wushkv_shared_prefixes, wushkv_prefix_attention
+ *                            the pages that sequences share at their start
+ *                            attended to once for all of them
+ *   wushkv_cross_attention   queries of other sequences, of any length, over
+ *                            whole stored ones
+ *   wushkv_weighted_attention, wushkv_evict_pages
+ *                            attention that adds up what each page receives,
+ *                            and the pages with the least that leave
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless marked (host), and must be
@@ -585,6 +593,138 @@ int wushkv_compact_pages(const wushkv_cache *c, const wushkv_pool *pool,
 
 /* Workspace of wushkv_compact_pages, or 0 for invalid arguments. */
 size_t wushkv_compact_workspace_bytes(const wushkv_cache *c);
+
+/*
+ * wushkv_shared_prefixes -- which sequences start with the same pages, from the
+ * page table (forks of one sequence do, wushkv_assign_pages).
+ *
+ *   min_pages  (host) >= 1: fewer pages than that are not worth sharing.
+ *   leader   int32 [batch], shared int32 [batch]: below.
+ *
+ * common(a, b) is the largest n, at most the number of complete pages of a and of
+ * b, for which the first n entries of their rows are the same and entry n - 1 is
+ * in the pool (0 if there is none); best(b) is the largest common(a, b) of all
+ * other sequences a.  Where best(b) >= min_pages, leader[b] is the lowest sequence
+ * a with a = b or common(a, b) >= best(b); shared[b] is best(b) if that is another
+ * sequence.  Everywhere else leader[b] is b and shared[b] 0 (a leader's own count
+ * is 0: wushkv_prefix_attention goes by those of the sequences that it leads).
+ */
+int wushkv_shared_prefixes(const wushkv_cache *c, int32_t min_pages, int32_t *leader, int32_t *shared,
+                           wushkv_stream_t stream);
+
+/*
+ * wushkv_prefix_attention -- wushkv_decode_attention for sequences that share
+ * pages at their start: a page that several have is read and attended to once for
+ * all of their query rows.
+ *
+ *   q, n_q_heads, t_k_inv, sm_scale, out  as wushkv_decode_attention takes them.
+ *   leader, shared  int32 [batch] device, as wushkv_shared_prefixes gives them.
+ *            Let s be shared[b], clamped to [0, the complete pages of both b and
+ *            leader[b]], or 0 where leader[b] is b or no sequence.  Sequence b
+ *            attends to the first s pages of leader[b]'s row, to its own pages
+ *            from s on, and to its windows.  A sequence whose own s is 0 and that
+ *            others name is attended to by the largest of theirs (its own pages
+ *            all the same, together with theirs).
+ *   workspace  wushkv_prefix_workspace_bytes() bytes, not initialised.
+ * A page that is not in the pool contributes nothing.  A sequence with seq_len 0
+ * gets zeros.  A batch above 1024 is WUSHKV_EUNSUPPORTED.
+ */
+int wushkv_prefix_attention(const wushkv_cache *c, const uint16_t *q, int32_t n_q_heads,
+                            const int32_t *leader, const int32_t *shared, const float *t_k_inv,
+                            float sm_scale, float *out, void *workspace, size_t workspace_bytes,
+                            wushkv_stream_t stream);
+
+/* Workspace of wushkv_prefix_attention, or 0 for invalid arguments. */
+size_t wushkv_prefix_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads);
+
+/*
+ * wushkv_cross_attention -- attention of query sequences over whole stored ones,
+ * of another length and without a mask: a decoder's queries over an encoder's
+ * states, which were appended to the cache as keys and values.
+ *
+ *   q        bf16 [n_seqs][max_tok][n_q_heads][head_dim]; heads as for
+ *            wushkv_decode_attention.
+ *   n_seqs   (host) query sequences, 1 to 1024.
+ *   n_tok    int32 [n_seqs] device, or NULL for max_tok everywhere: tokens of
+ *            each, clamped to [0, max_tok].
+ *   max_tok  (host) >= 1; n_seqs max_tok at most 262144.
+ *   source   int32 [n_seqs] device: the stored sequence that query sequence i
+ *            attends to (several may name the same: its pages are then read once
+ *            for 32 rows of them), or NULL for i (n_seqs at most the batch).
+ *   out      fp32 of q's shape.  Rows behind n_tok, of a source outside the batch
+ *            and of an empty one are zero.
+ *   t_k_inv, sm_scale  as wushkv_decode_attention takes them.
+ *   workspace  wushkv_cross_workspace_bytes() bytes, not initialised.
+ * Every token attends to all positions [0, seq_len[source[i]]).
+ */
+int wushkv_cross_attention(const wushkv_cache *c, const uint16_t *q, int32_t n_seqs,
+                           const int32_t *n_tok, int32_t max_tok, const int32_t *source,
+                           int32_t n_q_heads, const float *t_k_inv, float sm_scale, float *out,
+                           void *workspace, size_t workspace_bytes, wushkv_stream_t stream);
+
+/* Workspace of wushkv_cross_attention, or 0 for invalid arguments. */
+size_t wushkv_cross_workspace_bytes(const wushkv_cache *c, int32_t n_seqs, int32_t max_tok,
+                                    int32_t n_q_heads);
+
+/*
+ * wushkv_weighted_attention -- wushkv_sparse_attention, or over every page, that
+ * also adds up the attention weight of each page.
+ *
+ *   sel, n_sel, max_sel  the lists, as wushkv_sparse_attention takes them; or NULL,
+ *            NULL and -1: every page of the sequence.
+ *   weights  fp32 [batch][n_kv_heads][max_pages_per_seq], read and written: to the
+ *            entry of every page attended to is added the sum, over the group's
+ *            query heads and the page's positions, of the softmax's weights.  The
+ *            other entries are left as they are.
+ *   The other arguments are wushkv_decode_attention's; the workspace needs
+ *   wushkv_weighted_workspace_bytes().
+ * The caller zeroes a sequence's weights when it takes the slot for another one,
+ * and copies its source's for a fork.  A batch above 65535 is
+ * WUSHKV_EUNSUPPORTED.
+ */
+int wushkv_weighted_attention(const wushkv_cache *c, const uint16_t *q, int32_t n_q_heads,
+                              const int32_t *sel, const int32_t *n_sel, int32_t max_sel,
+                              const float *t_k_inv, float sm_scale, float *weights, float *out,
+                              void *workspace, size_t workspace_bytes, wushkv_stream_t stream);
+
+/* Workspace of wushkv_weighted_attention (max_sel -1: every page), or 0 for
+   invalid arguments. */
+size_t wushkv_weighted_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads, int32_t max_sel);
+
+/*
+ * wushkv_evict_pages -- complete pages with the least weight leave their
+ * sequences, which keep their length: the entries become -1, and the positions in
+ * them are attended to no more.
+ *
+ *   weights  fp32 [batch][n_kv_heads][max_pages_per_seq], as
+ *            wushkv_weighted_attention adds them up.
+ *   budget   int32 [batch] device: complete pages sequence b keeps at most; a
+ *            negative one leaves it as it is.
+ *   recent   (host) >= 0: a sequence's newest `recent` complete pages never leave
+ *            (so it may keep more than its budget).
+ *   table_out  int32 [batch][max_pages_per_seq], refs_out int32 [n_pages]: the new
+ *            page table and references; either may be the cache's, or the pool's,
+ *            own array (in place), and otherwise overlaps none of the call's.
+ *   sel, n_sel  nullable, both or neither: int32 [batch][n_kv_heads][max_sel] and
+ *            [batch][n_kv_heads]: the lists that the attentions take, of the pages
+ *            that are left, the one being filled among them, ascending and -1
+ *            behind, the same for every kv head; the newest max_sel where there
+ *            are more.
+ *   max_sel  (host) >= 0, the row length of sel.
+ *   evicted  int32 [batch]: pages that left.
+ *
+ * Of sequence b's row the entries in [0, held[b]) count.  score(page) is the sum
+ * of its weights over the kv heads, in fp64, rounded to fp32; one that is not a
+ * number counts as the largest.  Of the L complete pages in the pool those below
+ * the newest `recent` may leave: min(max(L - budget[b], 0), as many as there are)
+ * of them with the least score, of equal scores the lowest pages.  Each gives up one
+ * reference; pages without one are free.  pool->low stays right in both cases.
+ * The page table and the references must not be in use on another stream.
+ */
+int wushkv_evict_pages(const wushkv_cache *c, const wushkv_pool *pool, const float *weights,
+                       const int32_t *budget, int32_t recent, int32_t *table_out,
+                       int32_t *refs_out, int32_t *sel, int32_t *n_sel, int32_t max_sel,
+                       int32_t *evicted, wushkv_stream_t stream);
 
 /* Name of a status code. */
 const char *wushkv_status_string(int status);

@@ -29,6 +29,8 @@ __all__ = [
     "WushKVBounds", "WushKVPool", "wushkv_page_bounds", "wushkv_select_pages",
     "wushkv_select_workspace_bytes", "wushkv_sparse_attention", "wushkv_sparse_workspace_bytes",
     "wushkv_assign_pages", "wushkv_compact_pages", "wushkv_compact_workspace_bytes",
+    "wushkv_shared_prefixes", "wushkv_prefix_attention", "wushkv_prefix_workspace_bytes", "wushkv_cross_attention",
+    "wushkv_cross_workspace_bytes", "wushkv_weighted_attention", "wushkv_weighted_workspace_bytes", "wushkv_evict_pages",
     "PAGE_TOKENS",
     "header_functions",
 ]
@@ -639,6 +641,178 @@ def wushkv_compact_pages(cache: WushKVCache, pool: WushKVPool, bounds=None, tabl
         _check(dev, live_out, "live_out", torch.int32, (1,)), space[0], space[1], handle)
     check(st, "wushkv_compact_pages")
     return table_out, refs_out, live_out
+
+
+def wushkv_shared_prefixes(cache: WushKVCache, leader=None, shared=None, min_pages=1, stream=None):
+    """The pages that sequences have in common at their start, from the page
+    table: (leader, shared), int32 [batch] on the device, as
+    wushkv_prefix_attention takes them; prefixes of fewer than ``min_pages``
+    pages are left out.  They hold until a sequence that shares pages is freed
+    or forked, or loses one of them."""
+    torch = _torch()
+    dev, shape = cache.pages.get_device(), (cache.batch,)
+    min_pages = operator.index(min_pages)
+    handle = _launch_stream(dev, stream)
+    if leader is None:
+        leader = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
+    if shared is None:
+        shared = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
+    st = _lib.lib().wushkv_shared_prefixes(ctypes.byref(cache._desc), min_pages,
+                                           _check(dev, leader, "leader", torch.int32, shape),
+                                           _check(dev, shared, "shared", torch.int32, shape), handle)
+    check(st, "wushkv_shared_prefixes")
+    return leader, shared
+
+
+def _rows_call(name, q, out, workspace, need, stream):
+    """(out, its address, the workspace's address and bytes): those given, or new
+    ones; ``need`` gives the workspace's bytes, 0 where the call has no plan."""
+    torch = _torch()
+    if out is None:
+        out = _on_stream(torch.empty(q.shape, dtype=torch.float32, device=q.device), stream)
+    out_at = _check(q.get_device(), out, "out", torch.float32, q.shape)
+    if workspace is not None:
+        return out, out_at, _check_space(q.get_device(), workspace)
+    # (sizes without a plan: the call says what is wrong)
+    n = max(16, need())
+    workspace = _on_stream(torch.empty(n, dtype=torch.uint8, device=q.device), stream)
+    return out, out_at, (workspace.data_ptr(), n)
+
+
+def wushkv_prefix_workspace_bytes(cache: WushKVCache, n_q_heads: int) -> int:
+    return _lib.lib().wushkv_prefix_workspace_bytes(ctypes.byref(cache.desc), n_q_heads)
+
+
+def wushkv_prefix_attention(cache: WushKVCache, q, t_k_inv, leader, shared, sm_scale=None, out=None, workspace=None,
+                            stream=None):
+    """wushkv_decode_attention for sequences that share pages at their start,
+    which are attended to once for all of them: leader, shared int32 [batch]
+    (wushkv_shared_prefixes).  q: bf16 [batch][n_q][d]; t_k_inv: fp32
+    [n_kv][d][d].  Returns fp32 [batch][n_q][d]."""
+    torch = _torch()
+    dev = cache.pages.get_device()
+    b, hk, d = cache.batch, cache.n_kv_heads, cache.head_dim
+    n_q = q.shape[1] if q.dim() == 3 else 0
+    q_at = _check(dev, q, "q", torch.bfloat16, (b, n_q, d))
+    t_at = _check(dev, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    leader_at = _check(dev, leader, "leader", torch.int32, (b,))
+    shared_at = _check(dev, shared, "shared", torch.int32, (b,))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    handle = _launch_stream(dev, stream)
+    out, out_at, space = _rows_call("prefix", q, out, workspace, lambda: wushkv_prefix_workspace_bytes(cache, n_q), stream)
+    st = _lib.lib().wushkv_prefix_attention(ctypes.byref(cache._desc), q_at, n_q, leader_at, shared_at, t_at,
+                                            float(sm_scale), out_at, space[0], space[1], handle)
+    check(st, "wushkv_prefix_attention")
+    return out
+
+
+def wushkv_cross_workspace_bytes(cache: WushKVCache, n_seqs: int, max_tok: int, n_q_heads: int) -> int:
+    return _lib.lib().wushkv_cross_workspace_bytes(ctypes.byref(cache.desc), n_seqs, max_tok, n_q_heads)
+
+
+def wushkv_cross_attention(cache: WushKVCache, q, t_k_inv, n_tok=None, source=None, sm_scale=None, out=None,
+                           workspace=None, stream=None):
+    """Attention of query sequences over whole stored ones, without a mask (a
+    decoder's queries over an encoder's states).  q: bf16
+    [n_seqs][max_tok][n_q][d]; n_tok: int32 [n_seqs] on the device or None
+    (max_tok for all); source: int32 [n_seqs], the cache's sequence that each
+    attends to (several may name the same), or None (its own number).  Returns
+    fp32 [n_seqs][max_tok][n_q][d]."""
+    torch = _torch()
+    dev = cache.pages.get_device()
+    hk, d = cache.n_kv_heads, cache.head_dim
+    n_seqs, max_tok, n_q = q.shape[:3] if q.dim() == 4 else (0, 0, 0)
+    q_at = _check(dev, q, "q", torch.bfloat16, (n_seqs, max_tok, n_q, d))
+    t_at = _check(dev, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    n_at = None if n_tok is None else _check(dev, n_tok, "n_tok", torch.int32, (n_seqs,))
+    source_at = None if source is None else _check(dev, source, "source", torch.int32, (n_seqs,))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    handle = _launch_stream(dev, stream)
+    out, out_at, space = _rows_call("cross", q, out, workspace,
+                                    lambda: wushkv_cross_workspace_bytes(cache, n_seqs, max_tok, n_q), stream)
+    st = _lib.lib().wushkv_cross_attention(ctypes.byref(cache._desc), q_at, n_seqs, n_at, max_tok, source_at, n_q, t_at,
+                                           float(sm_scale), out_at, space[0], space[1], handle)
+    check(st, "wushkv_cross_attention")
+    return out
+
+
+def wushkv_weighted_workspace_bytes(cache: WushKVCache, n_q_heads: int, max_sel: int = -1) -> int:
+    return _lib.lib().wushkv_weighted_workspace_bytes(ctypes.byref(cache.desc), n_q_heads, max_sel)
+
+
+def wushkv_weighted_attention(cache: WushKVCache, q, t_k_inv, weights, sel=None, n_sel=None, sm_scale=None, out=None,
+                              workspace=None, stream=None):
+    """wushkv_sparse_attention over the listed pages (sel, n_sel), or over every
+    page where both are None, that adds each page's attention weight to
+    ``weights``, fp32 [batch][n_kv][max_pages].  Returns fp32 [batch][n_q][d]."""
+    torch = _torch()
+    dev = cache.pages.get_device()
+    b, hk, d = cache.batch, cache.n_kv_heads, cache.head_dim
+    n_q = q.shape[1] if q.dim() == 3 else 0
+    q_at = _check(dev, q, "q", torch.bfloat16, (b, n_q, d))
+    t_at = _check(dev, t_k_inv, "t_k_inv", torch.float32, (hk, d, d))
+    w_at = _check(dev, weights, "weights", torch.float32, (b, hk, cache.max_pages))
+    if (sel is None) != (n_sel is None):
+        raise ValueError("sel and n_sel go together")
+    max_sel, sel_at, n_at = -1, None, None
+    if sel is not None:
+        max_sel = sel.shape[2] if sel.dim() == 3 else 0
+        sel_at = _check(dev, sel, "sel", torch.int32, (b, hk, max_sel))
+        n_at = _check(dev, n_sel, "n_sel", torch.int32, (b, hk))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    handle = _launch_stream(dev, stream)
+    out, out_at, space = _rows_call("weighted", q, out, workspace,
+                                    lambda: wushkv_weighted_workspace_bytes(cache, n_q, max_sel), stream)
+    st = _lib.lib().wushkv_weighted_attention(ctypes.byref(cache._desc), q_at, n_q, sel_at, n_at, max_sel, t_at,
+                                              float(sm_scale), w_at, out_at, space[0], space[1], handle)
+    check(st, "wushkv_weighted_attention")
+    return out
+
+
+def wushkv_evict_pages(cache: WushKVCache, pool: WushKVPool, weights, budget, recent=0, max_sel=None, sel=None,
+                       n_sel=None, table_out=None, refs_out=None, evicted=None, stream=None):
+    """The complete pages with the least weight (fp32 [batch][n_kv][max_pages])
+    leave each sequence b that has more than budget[b] (int32 [batch]; negative:
+    as it is), but for its newest ``recent``.  The page table and references
+    change in place or, where table_out and refs_out are given, into those.
+    Returns (sel int32 [batch][n_kv][max_sel], the pages left, ascending, -1
+    behind; n_sel int32 [batch][n_kv]; evicted int32 [batch])."""
+    torch = _torch()
+    dev = cache.pages.get_device()
+    books = _pool_of(cache, dev, pool)
+    b, hk = cache.batch, cache.n_kv_heads
+    w_at = _check(dev, weights, "weights", torch.float32, (b, hk, cache.max_pages))
+    budget_at = _check(dev, budget, "budget", torch.int32, (b,))
+    if sel is not None:
+        if max_sel is not None and sel.shape[-1] != operator.index(max_sel):
+            raise ValueError("sel has another width than max_sel")
+        max_sel = sel.shape[2] if sel.dim() == 3 else 0
+    max_sel = cache.max_pages if max_sel is None else operator.index(max_sel)
+    handle = _launch_stream(dev, stream)
+    new = lambda *shape: _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)  # noqa: E731
+    if sel is None:
+        sel = new(b, hk, max(max_sel, 0))
+    if n_sel is None:
+        n_sel = new(b, hk)
+    if evicted is None:
+        evicted = new(b)
+    if table_out is None:
+        table_out = cache.page_table
+    if refs_out is None:
+        refs_out = pool.refs
+    sel_at = _check(dev, sel, "sel", torch.int32, (b, hk, max(max_sel, 0)))
+    st = _lib.lib().wushkv_evict_pages(
+        ctypes.byref(cache._desc), books, w_at, budget_at, operator.index(recent),
+        _check(dev, table_out, "table_out", torch.int32, (b, cache.max_pages)),
+        _check(dev, refs_out, "refs_out", torch.int32, (cache.n_pages,)),
+        # (a list of no entries has no address)
+        sel_at if max_sel > 0 else None, _check(dev, n_sel, "n_sel", torch.int32, (b, hk)) if max_sel > 0 else None, max_sel,
+        _check(dev, evicted, "evicted", torch.int32, (b,)), handle)
+    check(st, "wushkv_evict_pages")
+    return sel, n_sel, evicted
 
 
 def wushkv_wush_transform(m, h, gamma: float = 1e-2, t_out=None, t_inv_out=None,

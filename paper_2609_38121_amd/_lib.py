@@ -125,6 +125,22 @@ def _declare(L):
     L.wushkv_compact_pages.restype = ctypes.c_int
     L.wushkv_compact_workspace_bytes.argtypes = [D]
     L.wushkv_compact_workspace_bytes.restype = SZ
+    L.wushkv_shared_prefixes.argtypes = [D, I32, P, P, P]
+    L.wushkv_shared_prefixes.restype = ctypes.c_int
+    L.wushkv_prefix_attention.argtypes = [D, P, I32, P, P, P, F32, P, P, SZ, P]
+    L.wushkv_prefix_attention.restype = ctypes.c_int
+    L.wushkv_prefix_workspace_bytes.argtypes = [D, I32]
+    L.wushkv_prefix_workspace_bytes.restype = SZ
+    L.wushkv_cross_attention.argtypes = [D, P, I32, P, I32, P, I32, P, F32, P, P, SZ, P]
+    L.wushkv_cross_attention.restype = ctypes.c_int
+    L.wushkv_cross_workspace_bytes.argtypes = [D, I32, I32, I32]
+    L.wushkv_cross_workspace_bytes.restype = SZ
+    L.wushkv_weighted_attention.argtypes = [D, P, I32, P, P, I32, P, F32, P, P, P, SZ, P]
+    L.wushkv_weighted_attention.restype = ctypes.c_int
+    L.wushkv_weighted_workspace_bytes.argtypes = [D, I32, I32]
+    L.wushkv_weighted_workspace_bytes.restype = SZ
+    L.wushkv_evict_pages.argtypes = [D, O, P, P, I32, P, P, P, P, I32, P, P]
+    L.wushkv_evict_pages.restype = ctypes.c_int
     L.wushkv_read_probe.argtypes = [P, SZ, I32, P, P]
     L.wushkv_read_probe.restype = ctypes.c_int
     L.wushkv_quest_alpha.argtypes = [I32]

@@ -294,3 +294,50 @@ def compact(host, codes=None, scales=None):
             p = int(host.table[b, lp])
             host.table[b, lp] = to.get(p, p) if lp < host.held[b] and 0 <= p < host.n_pages else -1
     return n
+
+
+# ------------------------------------------------------------------ shared prefixes, eviction
+
+
+def shared_prefixes(host, min_pages=1):
+    """(leader, shared), pair by pair."""
+    def common(a, b):
+        n = 0
+        for i in range(min(host.complete(a), host.complete(b))):
+            if host.table[a, i] != host.table[b, i]:
+                break
+            if 0 <= host.table[a, i] < host.n_pages:
+                n = i + 1
+        return n
+    leader, shared = np.arange(host.b, dtype=np.int32), np.zeros(host.b, np.int32)
+    for b in range(host.b):
+        each = [0 if a == b else common(a, b) for a in range(host.b)]
+        if max(each) < min_pages:
+            continue
+        leader[b] = min(a for a in range(host.b) if a == b or each[a] >= max(each))
+        shared[b] = 0 if leader[b] == b else max(each)
+    return leader, shared
+
+
+def evict(host, weights, budget, recent, max_sel):
+    """In place on a Host; returns (sel, n_sel, evicted)."""
+    sel = np.full((host.b, host.hk, max_sel), -1, np.int32)
+    n_sel, gone = np.zeros((host.b, host.hk), np.int32), np.zeros(host.b, np.int32)
+    for b in range(host.b):
+        held = min(max(int(host.held[b]), 0), host.max_pages)
+        full, every = host.complete(b), host.every(b)
+        ok = [i for i in range(min(every, held)) if 0 <= host.table[b, i] < host.n_pages]
+        live = [i for i in ok if i < full]
+        free = [i for i in live if i < full - recent]
+        n = 0 if budget[b] < 0 else min(max(len(live) - int(budget[b]), 0), len(free))
+        with np.errstate(over="ignore"):
+            score = {i: np.float32(weights[b, :, i].astype(np.float64).sum()) for i in free}
+        for i in sorted(free, key=lambda i: (np.isnan(score[i]), score[i], i))[:n]:
+            host.refs[host.table[b, i]] -= 1
+            host.table[b, i] = -1
+            ok.remove(i)
+        gone[b] = n
+        ok = ok[max(0, len(ok) - max_sel):]
+        sel[b, :, :len(ok)] = ok
+        n_sel[b] = len(ok)
+    return sel, n_sel, gone
