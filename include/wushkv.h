@@ -647,7 +647,7 @@ size_t wushkv_prefix_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads);
  *   n_seqs   (host) query sequences, 1 to 1024.
  *   n_tok    int32 [n_seqs] device, or NULL for max_tok everywhere: tokens of
  *            each, clamped to [0, max_tok].
- *   max_tok  (host) >= 1; n_seqs max_tok at most 262144.
+ *   max_tok  (host) >= 1; n_seqs max_tok at most 131072.
  *   source   int32 [n_seqs] device: the stored sequence that query sequence i
  *            attends to (several may name the same: its pages are then read once
  *            for 32 rows of them), or NULL for i (n_seqs at most the batch).

@@ -14,16 +14,16 @@
 //   rows_merge_kernel / rows_join_kernel   what several workgroups have of a row,
 //                      merged; the pages' weights.
 //
-// Plan.  A tile is up to 32 query rows ((token, query head) pairs) with a run of a
+// Plan.  A tile is up to 16 query rows ((token, query head) pairs) with a run of a
 // stored sequence's pages and, where it is the rows' own sequence, its windows.
 // Prefix: a tile of its own pages and windows per sequence, and tiles of the
 // sequences that have a leader (sorted by what they share with it, longest first,
 // so that a tile's rows end at about the same page).  Cross: the tokens of all query
-// sequences of one stored sequence, 32 rows at a time.  The tiles' costs stand one
-// behind the other on a line, of which every workgroup takes the same share: a
-// workgroup may take a part of one tile or several tiles, and no length is known
-// to the host.  Within a workgroup the four waves take every fourth page each and
-// merge in LDS at the tile's end.
+// sequences of one stored sequence, 16 rows at a time.  Small tiles are dealt out
+// evenly, whole; the costs of the others stand one behind the other on a line, of
+// which every workgroup takes what it has room for beside its small ones: a part of
+// one tile or several tiles.  No length is known to the host.  Within a workgroup the
+// four waves take every fourth page each and merge in LDS at the tile's end.
 //
 // Pages.  As in decode_main_kernel, scores are scaled products of q~'s digit limbs
 // with the key codes, here with 16 query rows as the product's rows, one product a
@@ -38,17 +38,19 @@
 // (tiny scales would leave the lo parts no bits); sums of p z and p are fp32.
 //
 // Windows.  q~ and weights in three bf16 parts, 64 slots at a time.
+#include <algorithm>
 #include <atomic>
-#include <cfloat>
 
 #include "query.h"
 
 namespace wushkv {
 
 constexpr int kMaxRowItems = 1024;  // sequences that a plan sorts
-constexpr int kTileRows = 32;
+constexpr int kMaxWgs = 1024;       // workgroups of rows_kernel per kv head
+constexpr int kTileRows = 16;
+constexpr int kRowsPerCu = 2;  // workgroups of rows_kernel that a compute unit keeps
 
-// Tiles of one stored sequence's pages for up to 32 query rows.
+// Tiles of one stored sequence's pages for up to 16 query rows.
 struct RowTile {
     int32_t seq;             // whose page table, list and windows
     int32_t first, n_pages;  // page units: logical pages (or list entries) first ..
@@ -58,13 +60,13 @@ struct RowTile {
     int32_t limit;           // below it every row attends to a page
     int32_t part;            // its first partial row, -1: written out directly
     int32_t wg0, n_wg;       // workgroups that have a part of it
-    int64_t cost0;
+    int64_t cost0;           // its place on the line, -1: a small one
 };
 
 // Per kv head, at the start of its plan.
 struct RowPlan {
-    int64_t share, total;  // of a workgroup, of all tiles
-    int32_t n_tiles, pad[3];
+    int64_t total;  // the line's length
+    int32_t n_tiles, n_small;
 };
 
 enum { kPrefix = 0, kCross = 1, kWeighted = 2 };
@@ -92,8 +94,13 @@ struct RowsArgs {
     uint16_t *qpart;              // bf16 [n_kv][tokens][G][3][D]
     uint8_t *plan;                // per kv head plan_bytes
     int64_t plan_bytes;
-    int32_t wg_at, tile_at, tok_at, lim_at, map_at;  // offsets in a plan
+    // offsets in a plan: int64 [wgs + 1], where the workgroups' parts of the line begin;
+    // int32 [wgs], the tile there; the tiles; int32 [tiles], the small ones in order, and
+    // the costs before them; the token list and the tokens' limits; (tile, place) of each
+    // sequence with a leader
+    int32_t bound_at, wg_at, tile_at, small_at, before_at, tok_at, lim_at, map_at;
     int32_t wgs;                  // workgroups of rows_kernel per kv head
+    int32_t cus;                  // compute units
     int32_t reps;                 // 16-row groups a workgroup of rows_query_kernel takes
     float *part;                  // [n_kv][part_rows][D]
     float *part_ml;               // [n_kv][part_rows][2]
@@ -117,19 +124,27 @@ __device__ __forceinline__ int32_t quantised_end(const RowsArgs &a, int32_t b)
     return max(min(a.quant_end[b], a.seq_len[b]), a.s_sink);
 }
 
-// Costs of a page and of a window unit, by the rows' tiles of 16.
-__device__ __forceinline__ int32_t page_cost(int32_t rows) { return rows > 16 ? 3 : 2; }
-__device__ __forceinline__ int32_t window_cost(int32_t rows) { return 2 * page_cost(rows); }
-constexpr int64_t kLeastShare = 8;
+// Costs of a page and of a window unit.
+constexpr int32_t kPageCost = 3, kWindowCost = 6;
+constexpr int64_t kLeastShare = 24;
+// What a tile costs before its first unit.
+constexpr int32_t kTileCost = 24;
+__device__ __forceinline__ int64_t tile_cost(const RowTile &t)
+{
+    if (t.n_pages + t.n_win == 0) return 0;
+    return kTileCost + (int64_t)t.n_pages * kPageCost + (int64_t)t.n_win * kWindowCost;
+}
+// Tiles that are not cut.
+__device__ __forceinline__ bool is_small(const RowTile &t) { return t.n_pages + 2 * t.n_win <= 16; }
 
 // The unit that begins at or after place x of a tile's cost.
 __device__ __forceinline__ int32_t unit_at(const RowTile &t, int64_t x)
 {
-    const int32_t cp = page_cost(t.rows), cw = window_cost(t.rows);
+    x -= kTileCost;
     if (x <= 0) return 0;
-    const int64_t pages = (int64_t)t.n_pages * cp;
-    if (x <= pages) return (int32_t)((x + cp - 1) / cp);
-    const int64_t w = (x - pages + cw - 1) / cw;
+    const int64_t pages = (int64_t)t.n_pages * kPageCost;
+    if (x <= pages) return (int32_t)((x + kPageCost - 1) / kPageCost);
+    const int64_t w = (x - pages + kWindowCost - 1) / kWindowCost;
     return t.n_pages + (int32_t)(w < t.n_win ? w : t.n_win);
 }
 
@@ -159,55 +174,117 @@ __device__ __forceinline__ int64_t block_scan64(int64_t x, int64_t *sums, int64_
 struct PlanLds {
     int32_t group[kMaxRowItems], len[kMaxRowItems], most[kMaxRowItems], order[kMaxRowItems], flag[kMaxRowItems];
     int64_t sums[16];
+    int64_t bound[kMaxWgs + 1];
 };
 
-// The tiles' places on the line of costs, the workgroups' shares and the partial
+// The first w in [0, n) with bound[w] >= x (strict: > x), n if there is none.
+__device__ __forceinline__ int32_t bound_of(const int64_t *bound, int32_t n, int64_t x, bool strict)
+{
+    int32_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int32_t mid = (lo + hi) / 2;
+        if (strict ? bound[mid] > x : bound[mid] >= x) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// The tiles' places on the line of costs, the workgroups' parts of it and the partial
 // rows; all threads, after the tiles are written.
 __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_tiles, PlanLds &lds)
 {
     const int tid = threadIdx.x, nt = blockDim.x;
     RowTile *tiles = plan_part<RowTile>(a, h, a.tile_at);
     int32_t *wg_tile = plan_part<int32_t>(a, h, a.wg_at);
+    int32_t *small = plan_part<int32_t>(a, h, a.small_at), *before = plan_part<int32_t>(a, h, a.before_at);
+    const int32_t P = a.wgs;
     __syncthreads();
-    int64_t total = 0;
+    int64_t line = 0, smalls = 0;  // smalls: costs above, their number in the lower 16 bits
     for (int32_t t0 = 0; t0 < n_tiles; t0 += nt) {
         const int32_t t = t0 + tid;
         int64_t cost = 0;
-        if (t < n_tiles)
-            cost = (int64_t)tiles[t].n_pages * page_cost(tiles[t].rows) + (int64_t)tiles[t].n_win * window_cost(tiles[t].rows);
+        bool few = false;
+        if (t < n_tiles) {
+            const RowTile x = tiles[t];
+            cost = tile_cost(x);
+            few = is_small(x) && cost > 0;
+        }
         int64_t all;
-        const int64_t at = block_scan64(cost, lds.sums, all);
-        if (t < n_tiles) tiles[t].cost0 = total + at;
-        total += all;
+        const int64_t at = block_scan64(few ? 0 : cost, lds.sums, all);
+        if (t < n_tiles) tiles[t].cost0 = few ? -1 : line + at;
+        line += all;
+        const int64_t s = smalls + block_scan64(few ? (cost << 16) + 1 : 0, lds.sums, all);
+        if (few) {
+            small[s & 0xFFFF] = t;
+            before[s & 0xFFFF] = (int32_t)(s >> 16);
+        }
+        smalls += all;
     }
-    int64_t share = (total + a.wgs - 1) / a.wgs;
-    share = share > kLeastShare ? share : kLeastShare;
-    int64_t rows_before = 0;
+    const int32_t n_small = (int32_t)(smalls & 0xFFFF);
+    const int64_t cost_small = smalls >> 16;
+    int64_t most = (line + cost_small + P - 1) / P;
+    most = most > kLeastShare ? most : kLeastShare;
+    __syncthreads();  // (before is written)
+    auto first_small = [&](int32_t w) -> int32_t { return (int32_t)(((int64_t)w * n_small + P - 1) / P); };
+    auto cost_before = [&](int32_t i) -> int64_t { return i < n_small ? before[i] : cost_small; };
+    int64_t given = 0;
+    for (int32_t w0 = 0; w0 < P; w0 += nt) {
+        const int32_t w = w0 + tid;
+        int64_t room = 0;
+        if (w < P) {
+            const int64_t has = cost_before(first_small(w + 1)) - cost_before(first_small(w));
+            room = most > has ? most - has : 0;
+        }
+        int64_t all;
+        const int64_t at = given + block_scan64(room, lds.sums, all);
+        if (w < P) lds.bound[w] = at < line ? at : line;
+        given += all;
+    }
+    if (tid == 0) lds.bound[P] = line;
+    __syncthreads();
+    // a part of less than a tile's start and two pages goes to the neighbour
+    for (int32_t t0 = 0; t0 < n_tiles; t0 += nt) {
+        const int32_t t = t0 + tid;
+        if (t >= n_tiles) continue;
+        const RowTile x = tiles[t];
+        const int64_t end = x.cost0 + tile_cost(x);
+        if (x.cost0 < 0 || end == x.cost0) continue;
+        for (int32_t w = bound_of(lds.bound, P, x.cost0, true); w < P && lds.bound[w] < end; ++w) {
+            if (lds.bound[w] - x.cost0 <= kTileCost + 2 * kPageCost) lds.bound[w] = x.cost0;
+            else if (end - lds.bound[w] <= 2 * kPageCost) lds.bound[w] = end;
+        }
+    }
+    __syncthreads();
+    int64_t rows = 0;
     for (int32_t t0 = 0; t0 < n_tiles; t0 += nt) {
         const int32_t t = t0 + tid;
         int64_t need = 0;
-        int32_t w0 = 0, w1 = -1;
+        int32_t w0 = 0, n_wg = 0;
         if (t < n_tiles) {
-            const RowTile &x = tiles[t];
-            const int64_t cost = (int64_t)x.n_pages * page_cost(x.rows) + (int64_t)x.n_win * window_cost(x.rows);
-            if (cost > 0) {
-                w0 = (int32_t)(x.cost0 / share);
-                w1 = (int32_t)((x.cost0 + cost - 1) / share);
-                // the workgroups whose share begins in the tile
-                for (int32_t w = x.cost0 == (int64_t)w0 * share ? w0 : w0 + 1; w <= w1; ++w) wg_tile[w] = t;
+            const RowTile x = tiles[t];
+            const int64_t end = x.cost0 + tile_cost(x);
+            if (x.cost0 < 0) {
+                n_wg = 1;
+            } else if (end > x.cost0) {
+                w0 = bound_of(lds.bound, P, x.cost0, true) - 1;
+                const int32_t w1 = bound_of(lds.bound, P, end, false) - 1;
+                n_wg = w1 - w0 + 1;
+                for (int32_t w = bound_of(lds.bound, P, x.cost0, false); w <= w1; ++w) wg_tile[w] = t;
             }
-            if (!(a.mode == kCross && w1 <= w0)) need = (int64_t)(w1 - w0 + 1) * x.rows;
+            if (!(a.mode == kCross && n_wg == 1)) need = (int64_t)n_wg * x.rows;
         }
         int64_t all;
         const int64_t at = block_scan64(need, lds.sums, all);
         if (t < n_tiles) {
             tiles[t].wg0 = w0;
-            tiles[t].n_wg = w1 - w0 + 1;
-            tiles[t].part = need > 0 ? (int32_t)(rows_before + at) : -1;
+            tiles[t].n_wg = n_wg;
+            tiles[t].part = need > 0 ? (int32_t)(rows + at) : -1;
         }
-        rows_before += all;
+        rows += all;
     }
-    if (tid == 0) *plan_of(a, h) = RowPlan{share, total, n_tiles, {0, 0, 0}};
+    int64_t *bound = plan_part<int64_t>(a, h, a.bound_at);
+    for (int32_t w = tid; w <= P; w += nt) bound[w] = lds.bound[w];
+    if (tid == 0) *plan_of(a, h) = RowPlan{line, n_tiles, n_small};
 }
 
 __device__ __forceinline__ void plan_prefix(const RowsArgs &a, int h, PlanLds &lds)
@@ -444,17 +521,25 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
 
 // ------------------------------------------------------------------ the rows
 
-// Weights: at most 2^kGrow, about 2^kLift at a new maximum (fp16 holds nothing
-// below 2^-24, where the lo parts of small weights would be lost); the windows'
-// reference lies 2^kRoom above the maximum, so that sums of values near bf16's
-// largest stay finite.
-constexpr float kLift = 4.0f, kGrow = 8.0f, kRoom = 12.0f;
+// A page's weight p s is about 2^kLift where a row's maximum is new and the value
+// scale the largest (fp16 holds nothing below 2^-24, where the lo parts of small
+// weights would be lost), and at most 2^(kGrow + 1) later.  A window's reference lies
+// 2^kRoom above the maximum, so that sums of values near bf16's largest stay finite.
+constexpr float kLift = 4.0f, kGrow = 14.0f, kRoom = 12.0f;
+// Rows of weights in LDS: 64 tokens of two bytes, and room that spreads the rows read
+// together over the banks.
+constexpr int kPitch = 144;
 
-template <int D>
+// LDS: the rows' limbs, and a slice per wave, which holds its weights (two planes of
+// a page's, three of a window's) and in the end its sums.
+template <int D, int BITS>
 struct RowsLds {
-    static constexpr int kWave = kTileRows * D * 4 > 3 * kTileRows * 128 ? kTileRows * D * 4 : 3 * kTileRows * 128;
-    static constexpr int kMl = 4 * kWave;  // m, then l: float [4][32] each
-    static constexpr int kBytes = kMl + 2 * 4 * kTileRows * 4;
+    static constexpr int most(int a, int b) { return a > b ? a : b; }
+    static constexpr int kWave = most(16 * D * 4, 3 * 16 * kPitch);
+    static constexpr int kLimb = BITS == 2 ? 64 * 24 : 64 * 32;  // of 16 rows: [lane] 16 bytes, [lane] the rest
+    static constexpr int kMl = 4 * kWave + Limbs<BITS>::kCount * kLimb;  // m, then l: float [4][16] each
+    static constexpr int kBytes = kMl + 2 * 4 * 16 * 4;
+    __host__ __device__ static constexpr int limb_at(int l) { return 4 * kWave + l * kLimb; }
 };
 
 // Physical page of page unit i of stored sequence b, or -1; lp: its logical page.
@@ -466,6 +551,9 @@ __device__ __forceinline__ int32_t page_entry(const RowsArgs &a, int32_t b, int 
     return phys >= 0 && phys < a.n_pages ? phys : -1;
 }
 
+__device__ __forceinline__ _Float16 lo16(uint32_t x) { return __builtin_bit_cast(f16x2, x)[0]; }
+__device__ __forceinline__ _Float16 hi16(uint32_t x) { return __builtin_bit_cast(f16x2, x)[1]; }
+
 // The codes and parameters of a page as a lane holds them.
 template <int D, int BITS>
 struct PageRegs {
@@ -476,18 +564,18 @@ struct PageRegs {
     {
 #pragma unroll
         for (int i = 0; i < kKX; ++i)  // (at d = 64 the upper lanes' limbs are zero)
-            k[i] = *reinterpret_cast<const u32x4 *>(pg + 4 * L::k_word(lane % L::kKLanes, 4 * i));
+            k[i] = *reinterpret_cast<const u32x4 *>(pg + (uint32_t)(4 * L::k_word(lane % L::kKLanes, 4 * i)));
     }
     __device__ __forceinline__ void load_values(const uint8_t *pg, int lane)
     {
 #pragma unroll
         for (int i = 0; i < kVX; ++i)
-            v[i] = *reinterpret_cast<const u32x4 *>(pg + L::kRegionBytes + 4 * L::v_word(lane, 4 * i));
+            v[i] = *reinterpret_cast<const u32x4 *>(pg + (uint32_t)(L::kRegionBytes + 4 * L::v_word(lane, 4 * i)));
     }
     __device__ __forceinline__ void load_params(const uint8_t *pg, int n)
     {
-        kp = *reinterpret_cast<const u32x4 *>(pg + L::kParamOffset + 16 * n);
-        vp = *reinterpret_cast<const u32x4 *>(pg + L::kParamOffset + 4 * kPage + 16 * n);
+        kp = *reinterpret_cast<const u32x4 *>(pg + (uint32_t)(L::kParamOffset + 16 * n));
+        vp = *reinterpret_cast<const u32x4 *>(pg + (uint32_t)(L::kParamOffset + 4 * kPage + 16 * n));
     }
 };
 
@@ -499,116 +587,145 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
-// One tile of 16 rows: the running softmax of rows 4 j + r.
+// The running softmax of rows 4 j + r: a weight is 2^(logit - m).
 template <int D>
 struct RowState {
     f32x4 acc[D / 16];  // sums of p s 16 c (pages) or p v (windows), channels 16 nt + n
     f32x4 m, l, z;      // reference, sum of p, sum of p z (the lane's tokens)
 };
 
-// Moves the references up: the largest logit of each row over the wave's row of
-// lanes less lift.
+// Moves the references up, and what is relative to them.
 template <int D>
-__device__ __forceinline__ void raise_reference(RowState<D> &s, const f32x4 &top, float lift)
+__device__ __forceinline__ void move_references(RowState<D> &s, const f32x4 &up)
 {
+    const f32x4 f = {fexp2(-up[0]), fexp2(-up[1]), fexp2(-up[2]), fexp2(-up[3])};
+    s.m += up;
+    s.l *= f;
+    s.z *= f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float m_new = fmaxf(s.m[r], row_max16(top[r]) - lift);
-        const float f = fexp2(s.m[r] - m_new);
-        s.m[r] = m_new;
-        s.l[r] *= f;
-        s.z[r] *= f;
-#pragma unroll
-        for (int nt = 0; nt < D / 16; ++nt) s.acc[nt][r] *= f;
-    }
+    for (int nt = 0; nt < D / 16; ++nt) s.acc[nt] *= f;
 }
 
-template <int D, int BITS, int RT, bool WEIGH>
+// Moves the references of logits x, relative to them, so that a row's largest is at
+// most lift.  A row that sees none of the first tokens stays: it sees none later either.
+template <int D>
+__device__ __forceinline__ void raise_references(RowState<D> &s, f32x4 (&x)[4], float lift, bool fresh)
+{
+    f32x4 up;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) up[r] = row_max16(fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[2][r], x[3][r]))) - lift;
+    if (fresh) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) up[r] = up[r] == -INFINITY ? 0.0f : up[r];
+        s.m = up;
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) up[r] = fmaxf(up[r], 0.0f);
+        move_references<D>(s, up);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) x[t] -= up;
+}
+
+template <int D, int BITS, bool WEIGH>
 __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile, int32_t lo, int32_t hi, int32_t slot,
                                           uint8_t *lds, int h)
 {
     using L = Layout<D, BITS>;
     using LB = Limbs<BITS>;
+    using Lds = RowsLds<D, BITS>;
     constexpr int kNT = L::kNTiles, kC = L::kChunks, kScaleB = BITS == 2 ? 128 : 136;
-    constexpr int kPlane = RT * 16 * 128;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int j = lane >> 4, n = lane & 15;
+    constexpr int kPlane = 16 * kPitch;
+    // (the lane is opaque where a part begins, so that the addresses that follow from
+    // it are formed there, and do not hold registers from the kernel's start on)
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int lane = tid & 63;
+    asm volatile("" : "+v"(lane));
+    int j = lane >> 4, n = lane & 15;
     const int32_t G = 1 << a.g_log2, b = tile.seq;
     const int64_t rows_all = (int64_t)a.items * a.max_tok << a.g_log2;
     const int32_t *toks = plan_part<int32_t>(a, h, a.tok_at) + tile.tok;
     const int32_t S = a.seq_len[b], q_hi = quantised_end(a, b);
-    uint8_t *mine = lds + wave * RowsLds<D>::kWave;
-    const uint32_t pbuf = lds_addr(mine);
-    // (query row r of the tile, in the workspace's order)
-    auto row_at = [&](int r) -> int64_t { return h * rows_all + ((int64_t)toks[r >> a.g_log2] << a.g_log2) + (r & (G - 1)); };
+    const uint32_t pbuf = lds_addr(lds + wave * Lds::kWave);
+    // (query row r of the tile, in the workspace's order; behind them the last one again:
+    // what comes of it is not used, and no load waits in a branch)
+    auto row_at = [&](int r) -> int64_t {
+        const int i = min(r, tile.rows - 1);
+        return h * rows_all + ((int64_t)toks[i >> a.g_log2] << a.g_log2) + (i & (G - 1));
+    };
 
-    RowState<D> st[RT];
+    RowState<D> s;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-        for (int nt = 0; nt < kNT; ++nt) st[rt].acc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        st[rt].m = f32x4{-FLT_MAX, -FLT_MAX, -FLT_MAX, -FLT_MAX};
-        st[rt].l = st[rt].z = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int nt = 0; nt < kNT; ++nt) s.acc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    s.m = s.l = s.z = f32x4{0.f, 0.f, 0.f, 0.f};
+    bool fresh = true;  // nothing seen, references 0
     float unit = 1.0f;  // what acc is counted in
 
     const int32_t page_hi = min(hi, tile.n_pages);
     if (lo < page_hi) {
         // ============================================ pages
-        // operands: limb l of row 16 rt + n, and the digit sums by products with
-        // keys of code 1 (every column the same), from which the products start
-        i32x8 qa[RT][LB::kCount];
-        int sc03[RT], sc45[RT];
-        f32x4 zs[RT], from[RT];
+        // operands: limb l of row n, in LDS (beside the sums they would not fit
+        // the registers); a wave brings every fourth
+        const int64_t mine = row_at(n);
+        const u32x2 sc = *reinterpret_cast<const u32x2 *>(a.qaux + 4 * mine);
+        constexpr int kMine = (LB::kCount + 3) / 4;
+        u32x4 x0[kMine], x1[kMine];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int r = 16 * rt + n;
-            const int64_t row = r < tile.rows ? row_at(r) : -1;
-            sc03[rt] = sc45[rt] = 0x7F7F7F7F;
-            if (row >= 0) {
-                sc03[rt] = (int)a.qaux[4 * row];
-                sc45[rt] = (int)a.qaux[4 * row + 1];
-            }
-#pragma unroll
-            for (int l = 0; l < LB::kCount; ++l) {
-                u32x4 x0 = {0u, 0u, 0u, 0u}, x1 = x0;
-                if (row >= 0) {
-                    const uint8_t *src = a.qlimb + (row * kLimbRoom + l) * 128 + 32 * j;
-                    x0 = *reinterpret_cast<const u32x4 *>(src);
-                    if constexpr (BITS == 2) {
-                        const u32x2 y = *reinterpret_cast<const u32x2 *>(src + 16);
-                        x1 = u32x4{y[0], y[1], 0u, 0u};
-                    } else {
-                        x1 = *reinterpret_cast<const u32x4 *>(src + 16);
-                    }
-                }
-                qa[rt][l] = i32x8{(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
-            }
+        for (int k = 0; k < kMine; ++k) {
+            const int l = min(wave + 4 * k, LB::kCount - 1);
+            const u32x4 *src = reinterpret_cast<const u32x4 *>(a.qlimb + (mine * kLimbRoom + l) * 128 + 32 * j);
+            x0[k] = src[0];
+            x1[k] = src[1];
         }
-        auto products = [&](int rt, const i32x8 (&bop)[4], f32x4 (&c)[4]) {
-            limb_products<BITS, 0, kScaleB>(qa[rt][0], bop, sc03[rt], c);
-            limb_products<BITS, 1, kScaleB>(qa[rt][1], bop, sc03[rt], c);
-            limb_products<BITS, 2, kScaleB>(qa[rt][2], bop, sc03[rt], c);
-            limb_products<BITS, 3, kScaleB>(qa[rt][3], bop, sc03[rt], c);
-            limb_products<BITS, 4, kScaleB>(qa[rt][4], bop, sc45[rt], c);
-            if constexpr (LB::kCount > 5) limb_products<BITS, 5, kScaleB>(qa[rt][5], bop, sc45[rt], c);
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int l = min(wave + 4 * k, LB::kCount - 1);
+            uint8_t *to = lds + Lds::limb_at(l);
+            reinterpret_cast<u32x4 *>(to)[lane] = x0[k];
+            if constexpr (BITS == 2) reinterpret_cast<u32x2 *>(to + 1024)[lane] = u32x2{x1[k][0], x1[k][1]};
+            else reinterpret_cast<u32x4 *>(to + 1024)[lane] = x1[k];
+        }
+        __syncthreads();
+        const uint32_t limbs = lds_addr(lds);
+        auto limb = [&](int l) -> i32x8 {
+            const uint32_t at = limbs + Lds::limb_at(l);
+            const u32x4 x = lds_read16(at + 16 * lane);
+            if constexpr (BITS == 2) {
+                const u32x2 y = lds_read8(at + 1024 + 8 * lane);
+                return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], 0, 0};
+            } else {
+                const u32x4 y = lds_read16(at + 1024 + 16 * lane);
+                return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+            }
         };
+        auto products = [&](const i32x8 (&bop)[4], f32x4 (&c)[4]) {
+            limb_products<BITS, 0, kScaleB>(limb(0), bop, (int)sc[0], c);
+            limb_products<BITS, 1, kScaleB>(limb(1), bop, (int)sc[0], c);
+            limb_products<BITS, 2, kScaleB>(limb(2), bop, (int)sc[0], c);
+            limb_products<BITS, 3, kScaleB>(limb(3), bop, (int)sc[0], c);
+            limb_products<BITS, 4, kScaleB>(limb(4), bop, (int)sc[1], c);
+            if constexpr (LB::kCount > 5) limb_products<BITS, 5, kScaleB>(limb(5), bop, (int)sc[1], c);
+        };
+        // the digit sums, by products with keys of code 1 (every column the same), from
+        // which the products start
+        f32x4 zs;
         {
             const int one = BITS == 2 ? 0x11111111 : 0x01010101;
             const i32x8 o = BITS == 2 ? i32x8{one, one, one, one, 0, 0, 0, 0} : i32x8{one, one, one, one, one, one, one, one};
             const i32x8 ones[4] = {o, o, o, o};
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                f32x4 c[4] = {};
-                products(rt, ones, c);
-                zs[rt] = c[0];
-                from[rt] = c[0] * -a.mid;
-            }
+            f32x4 c[4] = {};
+            products(ones, c);
+            zs = c[0];
         }
         WidenNormal<BITS> wide;
         wide.init();
-        float vmul = 1.0f;      // a power of two that brings value scales to at most 8
-        uint32_t vmost = 0u;    // the largest scale that it serves (fp16 bits)
+        // where the lane writes its weights (rows 4 j + r, tokens 4 n ..) and reads the
+        // operand of row n (tokens 32 kc + 8 j ..)
+        const uint32_t pw = pbuf + 4 * j * kPitch + 8 * n, pr = pbuf + n * kPitch + 16 * j;
+        float grow = kGrow;
+        // value scales up to 2^vex are served: the references lie 2^vex higher
+        int vex = 0;
+        uint32_t vmost = 0u;    // the largest (fp16 bits)
 
         for (int32_t base = lo; base < page_hi; base += 256) {
             int32_t lp = -1, phys = -1;
@@ -635,6 +752,22 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 const int32_t nvalid = min(kPage, q_hi - (a.s_sink + clp * kPage));
                 const bool part = nvalid < kPage || clp >= tile.limit;
 
+                if (nvalid < kPage) {  // (whatever the page held before)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (4 * n + t >= nvalid) pg.vp[t] = 0u;
+                }
+                const uint32_t big = max(max(pg.vp[0] & 0x7FFFu, pg.vp[1] & 0x7FFFu), max(pg.vp[2] & 0x7FFFu, pg.vp[3] & 0x7FFFu));
+                if (__any(big > vmost)) {  // the largest scale lies in [2^(ex - 1), 2^ex)
+                    int ex;
+                    (void)frexpf(fminf(wave_max(f16_bits_to_f32(big)), 65504.0f), &ex);
+                    // (where there was no scale so far, down too)
+                    const float up = vmost == 0u ? -40.0f : (float)max(ex - vex, 0);
+                    if (!fresh) move_references<D>(s, f32x4{up, up, up, up});
+                    vex = ex;
+                    vmost = ex >= 16 ? 0x7FFFu : f32_to_f16_bits(ldexpf(2.0f, ex));  // (and twice that)
+                    grow = kGrow - (float)ex;
+                }
                 i32x8 bop[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
@@ -651,129 +784,91 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                                        (int)(w[3] & 0x0F0F0F0Fu), (int)((w[3] >> 4) & 0x0F0F0F0Fu)};
                     }
                 }
-                float ks[4], kz[4], vs[4], vz[4];
+                float mid[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) mid[t] = fmaf((float)lo16(pg.kp[t]), a.mid, (float)hi16(pg.kp[t]));
+                f32x4 each = {0.f, 0.f, 0.f, 0.f};
+                const f32x4 from = zs * -a.mid;
+                f32x4 x[4] = {from, from, from, from};
+                products(bop, x);
+                pg.load_keys(np, lane);
+                // logits, relative to the references: s (q~.(c - mid)) + ((z + mid s) sum(q~) - m)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        x[t][r] = fmaf((float)lo16(pg.kp[t]), x[t][r], fmaf(mid[t], zs[r], -s.m[r]));
                 if (part) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if (4 * n + t >= nvalid) pg.vp[t] = 0u;  // (whatever the page held before)
-                }
-                const uint32_t big = max(max(pg.vp[0] & 0x7FFFu, pg.vp[1] & 0x7FFFu), max(pg.vp[2] & 0x7FFFu, pg.vp[3] & 0x7FFFu));
-                if (__any(big > vmost)) {
-                    // the largest scale to between 1/2 and 1, with room for eight times that
-                    const float top = fminf(wave_max(f16_bits_to_f32(big)), 65504.0f);
-                    int ex;
-                    (void)frexpf(top, &ex);
-                    const float v_new = ldexpf(1.0f, -ex), f = v_new / vmul;
-                    vmul = v_new;
-                    vmost = f32_to_f16_bits(fminf(ldexpf(1.0f, ex + 3), 65504.0f));
-                    if (vmost >= 0x7BFFu) vmost = 0x7FFFu;
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int nt = 0; nt < kNT; ++nt) st[rt].acc[nt] *= f;
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    ks[t] = f16_bits_to_f32(pg.kp[t] & 0xFFFFu);
-                    kz[t] = fmaf(ks[t], a.mid, f16_bits_to_f32(pg.kp[t] >> 16));
-                    vs[t] = f16_bits_to_f32(pg.vp[t] & 0xFFFFu) * vmul;
-                    vz[t] = f16_bits_to_f32(pg.vp[t] >> 16);
-                }
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    RowState<D> &s = st[rt];
-                    f32x4 c[4] = {from[rt], from[rt], from[rt], from[rt]};
-                    products(rt, bop, c);
-                    if (rt + 1 == RT) {
-                        pg.load_keys(np, lane);
-                        pg.load_params(np, n);
-                    }
-                    f32x4 x[4];
-                    float most = -INFINITY;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[t][r] = fmaf(ks[t], c[t][r], fmaf(kz[t], zs[rt][r], -s.m[r]));
-                    // which of the rows and tokens are left out
-                    auto hide = [&](f32x4 (&y)[4]) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int row = 16 * rt + 4 * j + r;
-                            bool out = false;
-                            if (clp >= tile.limit && row < tile.rows)
-                                out = plan_part<int32_t>(a, h, a.lim_at)[tile.tok + (row >> a.g_log2)] <= clp;
-#pragma unroll
-                            for (int t = 0; t < 4; ++t)
-                                if (out || 4 * n + t >= nvalid) y[t][r] = -INFINITY;
-                        }
-                    };
-                    if (part) hide(x);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        most = fmaxf(fmaxf(most, fmaxf(x[t][0], x[t][1])), fmaxf(x[t][2], x[t][3]));
-                    if (__any(most > kGrow)) {
-                        f32x4 y[4];
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) y[t][r] = fmaf(ks[t], c[t][r], kz[t] * zs[rt][r]);
-                        if (part) hide(y);
-                        f32x4 top;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) top[r] = fmaxf(fmaxf(y[0][r], y[1][r]), fmaxf(y[2][r], y[3][r]));
-                        raise_reference<D>(s, top, kLift);
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) x[t][r] = y[t][r] - s.m[r];
-                    }
-                    f32x4 each = {0.f, 0.f, 0.f, 0.f};
+                    // the rows and tokens that are left out
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        f16x2 hi2[2], lo2[2];
-                        float p[4];
+                        const int row = 4 * j + r;
+                        bool out = false;
+                        if (clp >= tile.limit && row < tile.rows)
+                            out = plan_part<int32_t>(a, h, a.lim_at)[tile.tok + (row >> a.g_log2)] <= clp;
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) {
-                            p[t] = fexp2(x[t][r]);
-                            // (each part rounded from the exact product)
-                            const _Float16 ph = (_Float16)fmaf(p[t], vs[t], 0.0f);
-                            hi2[t >> 1][t & 1] = ph;
-                            lo2[t >> 1][t & 1] = (_Float16)fmaf(p[t], vs[t], -(float)ph);
-                            s.z[r] = fmaf(p[t], vz[t], s.z[r]);
-                        }
-                        each[r] = (p[0] + p[1]) + (p[2] + p[3]);
-                        s.l[r] += each[r];
-                        const int row = 16 * rt + 4 * j + r;
-                        lds_write8(pbuf + tbuf_at(row, 8 * n), __builtin_bit_cast(uint32_t, hi2[0]), __builtin_bit_cast(uint32_t, hi2[1]));
-                        lds_write8(pbuf + kPlane + tbuf_at(row, 8 * n), __builtin_bit_cast(uint32_t, lo2[0]), __builtin_bit_cast(uint32_t, lo2[1]));
+                        for (int t = 0; t < 4; ++t)
+                            if (out || 4 * n + t >= nvalid) x[t][r] = -INFINITY;
                     }
-                    if constexpr (WEIGH) {
-                        // what the page received, with the reference that it goes by
-                        float e = 0.0f, m = 0.0f;
+                }
+                float most = -INFINITY;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float t = row_sum16(each[r]);
-                            if (n == r) {
-                                e = t;
-                                m = s.m[r];
-                            }
+                for (int t = 0; t < 4; ++t)
+                    most = fmaxf(fmaxf(most, fmaxf(x[t][0], x[t][1])), fmaxf(x[t][2], x[t][3]));
+                if (fresh || __any(most > grow)) raise_references<D>(s, x, kLift - (float)vex, fresh);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t hi2[2], lo2[2];
+                    float p[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        p[t] = fexp2(x[t][r]);
+                        s.z[r] = fmaf(p[t], (float)hi16(pg.vp[t]), s.z[r]);
+                    }
+                    // each part is rounded from the exact product (the hi parts are opaque, so
+                    // that the lo parts read them where they are, two to a register)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float s0 = (float)lo16(pg.vp[2 * k]), s1 = (float)lo16(pg.vp[2 * k + 1]);
+                        const f16x2 ph = {(_Float16)fmaf(p[2 * k], s0, 0.0f), (_Float16)fmaf(p[2 * k + 1], s1, 0.0f)};
+                        hi2[k] = __builtin_bit_cast(uint32_t, ph);
+                        asm("" : "+v"(hi2[k]));
+                        const f16x2 hv = __builtin_bit_cast(f16x2, hi2[k]);
+                        const f16x2 pl = {(_Float16)fmaf(p[2 * k], s0, -(float)hv[0]),
+                                          (_Float16)fmaf(p[2 * k + 1], s1, -(float)hv[1])};
+                        lo2[k] = __builtin_bit_cast(uint32_t, pl);
+                    }
+                    const float sum = (p[0] + p[1]) + (p[2] + p[3]);
+                    if constexpr (WEIGH) each[r] = sum;
+                    s.l[r] += sum;
+                    lds_write8(pw + r * kPitch, hi2[0], hi2[1]);
+                    lds_write8(pw + kPlane + r * kPitch, lo2[0], lo2[1]);
+                }
+                fresh = false;
+                pg.load_params(np, n);
+                if constexpr (WEIGH) {
+                    // what the page received, with the reference that it goes by
+                    float e = 0.0f, m = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float t = row_sum16(each[r]);
+                        if (n == r) {
+                            e = t;
+                            m = s.m[r];
                         }
-                        const int row = 4 * j + n;
-                        if (rt == 0 && n < 4 && row < tile.rows) {
-                            const int64_t at = (((int64_t)h * a.batch + b) * a.max_sel + base + 4 * cur + wave) * G + row;
-                            reinterpret_cast<f32x2 *>(a.stat)[at] = f32x2{e, m};
-                        }
+                    }
+                    const int row = 4 * j + n;
+                    if (n < 4 && row < tile.rows) {
+                        const int64_t at = (((int64_t)h * a.batch + b) * a.max_sel + base + 4 * cur + wave) * G + row;
+                        reinterpret_cast<f32x2 *>(a.stat)[at] = f32x2{e, m};
                     }
                 }
                 wave_fence();
 #pragma unroll
                 for (int kc = 0; kc < 2; ++kc) {
-                    f16x8 A[RT][2];
+                    f16x8 A[2];
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int p = 0; p < 2; ++p)
-                            A[rt][p] = __builtin_bit_cast(f16x8, lds_read16(pbuf + p * kPlane + tbuf_at(16 * rt + n, 64 * kc + 16 * j)));
+                    for (int p = 0; p < 2; ++p) A[p] = __builtin_bit_cast(f16x8, lds_read16(pr + p * kPlane + 64 * kc));
 #pragma unroll
                     for (int uu = 0; uu < 2 * L::kNw; ++uu) {
                         const int w = kc * 2 * L::kNw + uu;
@@ -782,12 +877,10 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 #pragma unroll
                         for (int p = 0; p < 2; ++p)
 #pragma unroll
-                            for (int o = 0; o < L::kOpsPerWord; ++o)
-#pragma unroll
-                                for (int rt = 0; rt < RT; ++rt) {
-                                    f32x4 &acc = st[rt].acc[uu * L::kOpsPerWord + o];
-                                    acc = mfma16h(A[rt][p], as_op_h(op + 4 * o), acc);
-                                }
+                            for (int o = 0; o < L::kOpsPerWord; ++o) {
+                                f32x4 &acc = s.acc[uu * L::kOpsPerWord + o];
+                                acc = mfma16h(A[p], as_op_h(op + 4 * o), acc);
+                            }
                     }
                 }
                 wave_fence();
@@ -795,19 +888,22 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 cur = next;
             }
         }
-        unit = 0.0625f / vmul;
+        unit = 0.0625f;
     }
 
     if (hi > tile.n_pages) {
         // ============================================ windows
+        asm volatile("" : "+v"(lane));
+        j = lane >> 4;
+        n = lane & 15;
+        const uint32_t pw = pbuf + 4 * j * kPitch + 8 * n, pr = pbuf + n * kPitch + 16 * j;
         const int32_t ring = a.win_slots - a.s_sink;
         const int32_t a0 = S > q_hi ? (q_hi - a.s_sink) % ring : 0;
         const int32_t ring_live = S > q_hi ? S - q_hi : 0;
         const int64_t head = (int64_t)b * a.n_kv + h;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) st[rt].acc[nt] *= unit;
+        for (int nt = 0; nt < kNT; ++nt) s.acc[nt] *= unit;
+        const uint16_t *q = a.qpart + row_at(n) * 3 * D + 8 * j;
         unit = 1.0f;
         const int32_t from = max(lo, tile.n_pages);
         for (int32_t u = from + ((wave - (from - lo)) & 3); u < hi; u += 4) {
@@ -819,119 +915,119 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
             }
             const uint64_t live = __ballot(here);
             if (live == 0) continue;
+            // keys, queries and values are requested together each (the barriers hold the
+            // compiler to it: it would wait for one load after the other)
+            f32x4 c[4] = {};
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                RowState<D> &s = st[rt];
-                const int r0 = 16 * rt + n;
-                const int64_t row = r0 < tile.rows ? row_at(r0) : -1;
-                f32x4 c[4] = {};
+            for (int half = 0; half < kC; half += 2) {
+                bf16x8 kx[2][4], qp[2][3];
 #pragma unroll
-                for (int ch = 0; ch < kC; ++ch) {
-                    bf16x8 qp[3];
+                for (int ch = 0; ch < 2; ++ch) {
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) {
-                        u32x4 x = {0u, 0u, 0u, 0u};
-                        if (row >= 0) x = *reinterpret_cast<const u32x4 *>(a.qpart + (row * 3 + p) * D + 32 * ch + 8 * j);
-                        qp[p] = __builtin_bit_cast(bf16x8, x);
-                    }
+                    for (int t = 0; t < 4; ++t)
+                        kx[ch][t] = *reinterpret_cast<const bf16x8 *>(
+                            a.win_k + (head * a.win_slots + slot0 + 4 * n + t) * D + 32 * (half + ch) + 8 * j);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const bf16x8 kx = *reinterpret_cast<const bf16x8 *>(
-                            a.win_k + (head * a.win_slots + slot0 + 4 * n + t) * D + 32 * ch + 8 * j);
-#pragma unroll
-                        for (int p = 2; p >= 0; --p) c[t] = mfma16(qp[p], kx, c[t]);
-                    }
+                    for (int p = 0; p < 3; ++p)
+                        qp[ch][p] = *reinterpret_cast<const bf16x8 *>(q + p * D + 32 * (half + ch));
                 }
-                const uint32_t seen = (uint32_t)(live >> (4 * n)) & 15u;
-                f32x4 top = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                float most = -INFINITY;
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+                for (int ch = 0; ch < 2; ++ch)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (!((seen >> t) & 1u)) c[t][r] = -INFINITY;
-                        top[r] = fmaxf(top[r], c[t][r]);
-                        most = fmaxf(most, c[t][r] - s.m[r]);
-                    }
-                if (__any(most > -kRoom)) raise_reference<D>(s, top, -kRoom);
+                    for (int p = 2; p >= 0; --p)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) c[t] = mfma16(qp[ch][p], kx[ch][t], c[t]);
+            }
+            u32x4 vy[kNT];
+            auto load_values = [&](int kc) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt)
+                    vy[nt] = *reinterpret_cast<const u32x4 *>(
+                        a.win_v + (head * D + 16 * nt + n) * a.win_slots + slot0 + 32 * kc + 8 * j);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            load_values(0);
+            const uint32_t seen = (uint32_t)(live >> (4 * n)) & 15u;
+            float most = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int at = 16 * rt + 4 * j + r;
-                    float p[4];
+                    c[t][r] = (seen >> t) & 1u ? c[t][r] - s.m[r] : -INFINITY;
+                    most = fmaxf(most, c[t][r]);
+                }
+            if (fresh || __any(most > -kRoom)) raise_references<D>(s, c, -kRoom, fresh);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) p[t] = fexp2(c[t][r] - s.m[r]);
-                    s.l[r] += (p[0] + p[1]) + (p[2] + p[3]);
+            for (int r = 0; r < 4; ++r) {
+                float p[4];
 #pragma unroll
-                    for (int q = 0; q < 3; ++q) {
-                        const uint32_t u0 = pack_bf16_rne(p[0], p[1]), u1 = pack_bf16_rne(p[2], p[3]);
-                        lds_write8(pbuf + q * kPlane + tbuf_at(at, 8 * n), u0, u1);
-                        p[0] -= bf16_bits_to_f32(u0 & 0xFFFFu);
-                        p[1] -= bf16_bits_to_f32(u0 >> 16);
-                        p[2] -= bf16_bits_to_f32(u1 & 0xFFFFu);
-                        p[3] -= bf16_bits_to_f32(u1 >> 16);
-                    }
+                for (int t = 0; t < 4; ++t) p[t] = fexp2(c[t][r]);
+                s.l[r] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    const uint32_t u0 = pack_bf16_rne(p[0], p[1]), u1 = pack_bf16_rne(p[2], p[3]);
+                    lds_write8(pw + (16 * q + r) * kPitch, u0, u1);
+                    p[0] -= bf16_bits_to_f32(u0 & 0xFFFFu);
+                    p[1] -= bf16_bits_to_f32(u0 >> 16);
+                    p[2] -= bf16_bits_to_f32(u1 & 0xFFFFu);
+                    p[3] -= bf16_bits_to_f32(u1 >> 16);
                 }
             }
             wave_fence();
 #pragma unroll
             for (int kc = 0; kc < 2; ++kc) {
-                bf16x8 A[RT][3];
+                bf16x8 A[3];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int p = 0; p < 3; ++p)
-                        A[rt][p] = __builtin_bit_cast(bf16x8, lds_read16(pbuf + p * kPlane + tbuf_at(16 * rt + n, 64 * kc + 16 * j)));
+                for (int p = 0; p < 3; ++p)
+                    A[p] = __builtin_bit_cast(bf16x8, lds_read16(pr + 16 * p * kPitch + 64 * kc));
+                if (kc == 1) load_values(kc);
                 // dead slots' values are zeroed, whatever bits they hold
                 const uint32_t bits = (uint32_t)(live >> (32 * kc + 8 * j)) & 255u;
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
-                    u32x4 y = *reinterpret_cast<const u32x4 *>(
-                        a.win_v + (head * D + 16 * nt + n) * a.win_slots + slot0 + 32 * kc + 8 * j);
+                    u32x4 y = vy[nt];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         y[i] &= (((bits >> (2 * i)) & 1u) ? 0x0000FFFFu : 0u) | (((bits >> (2 * i + 1)) & 1u) ? 0xFFFF0000u : 0u);
 #pragma unroll
-                    for (int p = 2; p >= 0; --p)
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt)
-                            st[rt].acc[nt] = mfma16(A[rt][p], __builtin_bit_cast(bf16x8, y), st[rt].acc[nt]);
+                    for (int p = 2; p >= 0; --p) s.acc[nt] = mfma16(A[p], __builtin_bit_cast(bf16x8, y), s.acc[nt]);
                 }
             }
             wave_fence();
+            fresh = false;
         }
     }
 
     // ---- the four waves' results, merged
-    float(*o)[D] = reinterpret_cast<float(*)[D]>(mine);
-    float *sm = reinterpret_cast<float *>(lds + RowsLds<D>::kMl), *sl = sm + 4 * kTileRows;
+    float(*o)[D] = reinterpret_cast<float(*)[D]>(lds + wave * Lds::kWave);
+    float *sm = reinterpret_cast<float *>(lds + Lds::kMl), *sl = sm + 4 * 16;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int r = 0; r < 4; ++r) {
+        const int row = 4 * j + r;
+        const float z = row_sum16(s.z[r]), l = row_sum16(s.l[r]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = 16 * rt + 4 * j + r;
-            const float z = row_sum16(st[rt].z[r]), l = row_sum16(st[rt].l[r]);
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) o[row][16 * nt + n] = fmaf(st[rt].acc[nt][r], unit, z);
-            if (n == 0) {
-                sm[wave * kTileRows + row] = st[rt].m[r] == -FLT_MAX ? -INFINITY : st[rt].m[r];
-                sl[wave * kTileRows + row] = l;
-            }
+        for (int nt = 0; nt < kNT; ++nt) o[row][16 * nt + n] = fmaf(s.acc[nt][r], unit, z);
+        if (n == 0) {
+            sm[wave * 16 + row] = l == 0.0f ? -INFINITY : s.m[r];  // (none: no token seen)
+            sl[wave * 16 + row] = l;
         }
+    }
     __syncthreads();
     for (int i = tid; i < tile.rows * (D / 4); i += 256) {
         const int r = i / (D / 4), c = i % (D / 4);
         float mx = -INFINITY, l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w * kTileRows + r]);
+        for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w * 16 + r]);
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (mx != -INFINITY) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float m = sm[w * kTileRows + r];
+                const float m = sm[w * 16 + r];
                 if (m == -INFINITY) continue;
                 const float f = fexp2(m - mx);
-                l = fmaf(f, sl[w * kTileRows + r], l);
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(lds + w * RowsLds<D>::kWave + (r * D + 4 * c) * 4);
+                l = fmaf(f, sl[w * 16 + r], l);
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(lds + w * Lds::kWave + (r * D + 4 * c) * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[e], x[e]);
             }
@@ -951,22 +1047,44 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 }
 
 template <int D, int BITS, bool WEIGH>
-__global__ void __launch_bounds__(256, 2) rows_kernel(RowsArgs a)
+__global__ void __launch_bounds__(256, kRowsPerCu) rows_kernel(RowsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[RowsLds<D>::kBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[RowsLds<D, BITS>::kBytes];
     const int h = blockIdx.x, w = blockIdx.y;
     const RowPlan plan = *plan_of(a, h);
-    const int64_t begin = w * plan.share, end = begin + plan.share;
-    if (begin >= plan.total) return;
+    const int64_t *bound = plan_part<const int64_t>(a, h, a.bound_at);
+    const int32_t *small = plan_part<const int32_t>(a, h, a.small_at);
+    const int64_t begin = bound[w], end = bound[w + 1];
     const RowTile *tiles = plan_part<const RowTile>(a, h, a.tile_at);
-    for (int32_t t = plan_part<const int32_t>(a, h, a.wg_at)[w]; t < plan.n_tiles; ++t) {
-        const RowTile tile = tiles[t];
-        if (tile.cost0 >= end) break;
-        if (tile.n_wg == 0) continue;
-        const int32_t lo = unit_at(tile, begin - tile.cost0), hi = unit_at(tile, end - tile.cost0);
-        const int32_t slot = tile.part < 0 ? -1 : tile.part + (w - tile.wg0) * tile.rows;
-        if (!WEIGH && tile.rows > 16) take_tile<D, BITS, 2, false>(a, tile, lo, hi, slot, lds, h);
-        else take_tile<D, BITS, 1, WEIGH>(a, tile, lo, hi, slot, lds, h);
+    // its small tiles (latencies, mostly) and its part of the line, every other
+    // workgroup of a compute unit the other way round
+    int32_t s = (int32_t)(((int64_t)w * plan.n_small + a.wgs - 1) / a.wgs);
+    const int32_t s1 = (int32_t)(((int64_t)(w + 1) * plan.n_small + a.wgs - 1) / a.wgs);
+    int32_t t = begin < plan.total ? plan_part<const int32_t>(a, h, a.wg_at)[w] : plan.n_tiles;
+    const bool late = ((h + a.n_kv * w) / a.cus) & 1;
+    for (;;) {
+        RowTile tile;
+        int32_t lo, hi, slot;
+        if (s < s1 && !(late && t < plan.n_tiles)) {
+            tile = tiles[small[s++]];
+            lo = 0;
+            hi = tile.n_pages + tile.n_win;
+            slot = tile.part;
+        } else if (t < plan.n_tiles) {
+            tile = tiles[t++];
+            if (tile.cost0 < 0 || tile.n_wg == 0) continue;
+            if (tile.cost0 >= end) {
+                t = plan.n_tiles;
+                continue;
+            }
+            // (a workgroup without room in the midst of a tile: nothing of it)
+            lo = unit_at(tile, begin - tile.cost0);
+            hi = unit_at(tile, end - tile.cost0);
+            slot = tile.part < 0 ? -1 : tile.part + (w - tile.wg0) * tile.rows;
+        } else {
+            break;
+        }
+        take_tile<D, BITS, WEIGH>(a, tile, lo, hi, slot, lds, h);
     }
 }
 
@@ -1071,17 +1189,17 @@ __global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a)
 {
     const int h = blockIdx.x, w = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int32_t G = 1 << a.g_log2;
-    const RowPlan plan = *plan_of(a, h);
-    if ((w + 1) * plan.share >= plan.total) return;
+    const int64_t at = plan_part<const int64_t>(a, h, a.bound_at)[w + 1];
+    if (at >= plan_of(a, h)->total) return;
     const RowTile tile = plan_part<const RowTile>(a, h, a.tile_at)[plan_part<const int32_t>(a, h, a.wg_at)[w + 1]];
-    if (tile.wg0 != w || tile.n_wg < 2) return;
+    if (tile.cost0 == at || tile.wg0 != w) return;
     const int32_t *toks = plan_part<const int32_t>(a, h, a.tok_at) + tile.tok;
     for (int r = wave; r < tile.rows; r += 4) {
         float o[D / 64], M, l;
         merge_row<D>(a, h, tile.n_wg, [&](int i) -> int64_t { return tile.part + (int64_t)i * tile.rows + r; }, o, M, l);
-        const int64_t at = (((int64_t)toks[r >> a.g_log2] * a.n_kv + h) << a.g_log2) + (r & (G - 1));
+        const int64_t to = (((int64_t)toks[r >> a.g_log2] * a.n_kv + h) << a.g_log2) + (r & (G - 1));
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) a.out[at * D + (D / 64) * lane + e] = l != 0.0f ? o[e] / l : 0.0f;
+        for (int e = 0; e < D / 64; ++e) a.out[to * D + (D / 64) * lane + e] = l != 0.0f ? o[e] / l : 0.0f;
     }
 }
 
@@ -1120,7 +1238,8 @@ static int64_t lay_out(const wushkv_cache *c, int32_t mode, int32_t n_q, int64_t
         at += (bytes + 255) / 256 * 256;
         return ws + was;
     };
-    a.wgs = (int32_t)(2 * compute_units() / hk > 1 ? 2 * compute_units() / hk : 1);
+    a.cus = (int32_t)compute_units();
+    a.wgs = (int32_t)std::min<int64_t>(std::max<int64_t>(kRowsPerCu * compute_units() / hk, 1), kMaxWgs);
     // (cross: a stored sequence's last tile may be short)
     const int64_t tiles = mode == kPrefix ? 2 * B : mode == kWeighted ? B : (tokens * G + kTileRows - 1) / kTileRows + (items < B ? items : B);
     a.part_rows = mode == kPrefix ? 2 * B * G + kTileRows * (int64_t)a.wgs
@@ -1137,8 +1256,11 @@ static int64_t lay_out(const wushkv_cache *c, int32_t mode, int32_t n_q, int64_t
         p += (bytes + 15) / 16 * 16;
         return (int32_t)was;
     };
-    a.wg_at = within(4 * ((int64_t)a.wgs + 1));
+    a.bound_at = within(8 * ((int64_t)a.wgs + 1));
+    a.wg_at = within(4 * (int64_t)a.wgs);
     a.tile_at = within(sizeof(RowTile) * tiles);
+    a.small_at = within(4 * tiles);
+    a.before_at = within(4 * tiles);
     a.tok_at = within(4 * (mode == kPrefix ? 2 * B : tokens));
     a.lim_at = within(mode == kPrefix ? 8 * B : 0);
     a.map_at = within(mode == kPrefix ? 8 * B : 0);
@@ -1244,7 +1366,7 @@ static int check_cross(const wushkv_cache *c, int32_t n_seqs, int32_t max_tok, i
     if (st != WUSHKV_OK) return st;
     if (n_seqs < 1 || max_tok < 1) return WUSHKV_EINVAL;
     // (tokens and their rows are counted in 32 bits, their groups in a grid)
-    if (n_seqs > kMaxRowItems || (int64_t)n_seqs * max_tok > (1 << 18)) return WUSHKV_EUNSUPPORTED;
+    if (n_seqs > kMaxRowItems || (int64_t)n_seqs * max_tok > (1 << 17)) return WUSHKV_EUNSUPPORTED;
     return WUSHKV_OK;
 }
 
