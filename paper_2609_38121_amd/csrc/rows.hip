@@ -47,7 +47,8 @@ namespace wushkv {
 
 constexpr int kMaxRowItems = 1024;  // sequences that a plan sorts
 constexpr int kMaxWgs = 1024;       // workgroups of rows_kernel per kv head
-constexpr int kTileRows = 16;
+constexpr int kTileLog2 = 4, kTileRows = 1 << kTileLog2;
+constexpr int kReps = 4;        // most 16-row groups that a workgroup of rows_query_kernel takes
 constexpr int kRowsPerCu = 2;  // workgroups of rows_kernel that a compute unit keeps
 
 // Tiles of one stored sequence's pages for up to 16 query rows.
@@ -100,6 +101,7 @@ struct RowsArgs {
     // sequence with a leader
     int32_t bound_at, wg_at, tile_at, small_at, before_at, tok_at, lim_at, map_at;
     int32_t wgs;                  // workgroups of rows_kernel per kv head
+    uint64_t inverse;             // 2^64 / wgs, rounded up (at most 2^64 - 1)
     int32_t cus;                  // compute units
     int32_t reps;                 // 16-row groups a workgroup of rows_query_kernel takes
     float *part;                  // [n_kv][part_rows][D]
@@ -124,15 +126,16 @@ __device__ __forceinline__ int32_t quantised_end(const RowsArgs &a, int32_t b)
     return max(min(a.quant_end[b], a.seq_len[b]), a.s_sink);
 }
 
-// Costs of a page and of a window unit.
-constexpr int32_t kPageCost = 3, kWindowCost = 6;
-constexpr int64_t kLeastShare = 24;
-// What a tile costs before its first unit.
-constexpr int32_t kTileCost = 24;
+// Costs of a page, of a window unit and of a tile before its first unit (powers of two
+// and shifts: the plan and a tile's start run once, and are as long as their code, which
+// is seldom in the caches).
+constexpr int kPageShift = 2, kWindowShift = 4;
+constexpr int32_t kTileCost = 36;
+constexpr int64_t kLeastShare = 32;
 __device__ __forceinline__ int64_t tile_cost(const RowTile &t)
 {
     if (t.n_pages + t.n_win == 0) return 0;
-    return kTileCost + (int64_t)t.n_pages * kPageCost + (int64_t)t.n_win * kWindowCost;
+    return kTileCost + ((int64_t)t.n_pages << kPageShift) + ((int64_t)t.n_win << kWindowShift);
 }
 // Tiles that are not cut.
 __device__ __forceinline__ bool is_small(const RowTile &t) { return t.n_pages + 2 * t.n_win <= 16; }
@@ -142,40 +145,61 @@ __device__ __forceinline__ int32_t unit_at(const RowTile &t, int64_t x)
 {
     x -= kTileCost;
     if (x <= 0) return 0;
-    const int64_t pages = (int64_t)t.n_pages * kPageCost;
-    if (x <= pages) return (int32_t)((x + kPageCost - 1) / kPageCost);
-    const int64_t w = (x - pages + kWindowCost - 1) / kWindowCost;
+    const int64_t pages = (int64_t)t.n_pages << kPageShift;
+    if (x <= pages) return (int32_t)((x + (1 << kPageShift) - 1) >> kPageShift);
+    const int64_t w = (x - pages + (1 << kWindowShift) - 1) >> kWindowShift;
     return t.n_pages + (int32_t)(w < t.n_win ? w : t.n_win);
 }
 
-// Exclusive prefix sum over the workgroup's threads, and the total.
-__device__ __forceinline__ int64_t block_scan64(int64_t x, int64_t *sums, int64_t &total)
+// Exclusive prefix sums over the workgroup's threads, and the totals.
+struct Pair {
+    int64_t a, b;
+};
+__device__ __forceinline__ Pair block_scan(Pair x, Pair *sums, Pair &total)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
-    int64_t in = x;
-#pragma unroll
+    Pair in = x;
+#pragma unroll 1
     for (int s = 1; s < 64; s <<= 1) {
-        const int64_t y = __shfl_up(in, s);
-        if (lane >= s) in += y;
+        const int64_t ya = __shfl_up(in.a, s), yb = __shfl_up(in.b, s);
+        if (lane >= s) in = Pair{in.a + ya, in.b + yb};
     }
     __syncthreads();  // the last call's sums are read
     if (lane == 63) sums[wave] = in;
     __syncthreads();
-    int64_t before = 0, all = 0;
+    Pair before{0, 0}, all{0, 0};
+#pragma unroll 1
     for (int w = 0; w < waves; ++w) {
-        const int64_t v = sums[w];
-        if (w < wave) before += v;
-        all += v;
+        const Pair v = sums[w];
+        if (w < wave) before = Pair{before.a + v.a, before.b + v.b};
+        all = Pair{all.a + v.a, all.b + v.b};
     }
     total = all;
-    return before + in - x;
+    return Pair{before.a + in.a - x.a, before.b + in.b - x.b};
+}
+__device__ __forceinline__ int64_t block_scan(int64_t x, Pair *sums, int64_t &total)
+{
+    Pair all;
+    const int64_t before = block_scan(Pair{x, 0}, sums, all).a;
+    total = all.a;
+    return before;
 }
 
 struct PlanLds {
-    int32_t group[kMaxRowItems], len[kMaxRowItems], most[kMaxRowItems], order[kMaxRowItems], flag[kMaxRowItems];
-    int64_t sums[16];
+    int2 item[kMaxRowItems];  // leader or stored sequence (-1: none); pages shared or tokens
+    int32_t most[kMaxRowItems], order[kMaxRowItems], flag[kMaxRowItems], at[kMaxRowItems], sum[kMaxRowItems], count;
+    Pair sums[8];
     int64_t bound[kMaxWgs + 1];
 };
+
+// The first of n small tiles that workgroup w takes: w n / wgs, rounded up to a place
+// near it.
+__device__ __forceinline__ int32_t small_of(const RowsArgs &a, int32_t w, int32_t n)
+{
+    // (w <= 1024, n <= 2^17; inverse is 2^64 / wgs rounded up: exactly n for the last)
+    const int32_t at = (int32_t)__umul64hi((uint64_t)((uint32_t)w * (uint32_t)n), a.inverse);
+    return at < n && w < a.wgs ? at : n;
+}
 
 // The first w in [0, n) with bound[w] >= x (strict: > x), n if there is none.
 __device__ __forceinline__ int32_t bound_of(const int64_t *bound, int32_t n, int64_t x, bool strict)
@@ -199,33 +223,38 @@ __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_ti
     int32_t *small = plan_part<int32_t>(a, h, a.small_at), *before = plan_part<int32_t>(a, h, a.before_at);
     const int32_t P = a.wgs;
     __syncthreads();
-    int64_t line = 0, smalls = 0;  // smalls: costs above, their number in the lower 16 bits
+    RowTile mine{};  // the first of the thread's tiles (mostly its only one) stays in registers
+    if (tid < n_tiles) mine = tiles[tid];
+    auto tile_at = [&](int32_t t) -> RowTile { return t == tid ? mine : tiles[t]; };
+    int64_t line = 0, smalls = 0;  // smalls: costs above, their number in the lower 17 bits
     for (int32_t t0 = 0; t0 < n_tiles; t0 += nt) {
         const int32_t t = t0 + tid;
         int64_t cost = 0;
         bool few = false;
         if (t < n_tiles) {
-            const RowTile x = tiles[t];
+            const RowTile x = tile_at(t);
             cost = tile_cost(x);
             few = is_small(x) && cost > 0;
         }
-        int64_t all;
-        const int64_t at = block_scan64(few ? 0 : cost, lds.sums, all);
-        if (t < n_tiles) tiles[t].cost0 = few ? -1 : line + at;
-        line += all;
-        const int64_t s = smalls + block_scan64(few ? (cost << 16) + 1 : 0, lds.sums, all);
+        Pair all;
+        const Pair at = block_scan(Pair{few ? 0 : cost, few ? (cost << 17) + 1 : 0}, lds.sums, all);
+        const int64_t cost0 = few ? -1 : line + at.a;
+        if (t < n_tiles) tiles[t].cost0 = cost0;
+        if (t == tid) mine.cost0 = cost0;
         if (few) {
-            small[s & 0xFFFF] = t;
-            before[s & 0xFFFF] = (int32_t)(s >> 16);
+            const int64_t s = smalls + at.b;
+            small[s & 0x1FFFF] = t;
+            before[s & 0x1FFFF] = (int32_t)(s >> 17);
         }
-        smalls += all;
+        line += all.a;
+        smalls += all.b;
     }
-    const int32_t n_small = (int32_t)(smalls & 0xFFFF);
-    const int64_t cost_small = smalls >> 16;
-    int64_t most = (line + cost_small + P - 1) / P;
+    const int32_t n_small = (int32_t)(smalls & 0x1FFFF);
+    const int64_t cost_small = smalls >> 17;
+    int64_t most = (int64_t)__umul64hi((uint64_t)(line + cost_small), a.inverse) + 1;
     most = most > kLeastShare ? most : kLeastShare;
     __syncthreads();  // (before is written)
-    auto first_small = [&](int32_t w) -> int32_t { return (int32_t)(((int64_t)w * n_small + P - 1) / P); };
+    auto first_small = [&](int32_t w) -> int32_t { return small_of(a, w, n_small); };
     auto cost_before = [&](int32_t i) -> int64_t { return i < n_small ? before[i] : cost_small; };
     int64_t given = 0;
     for (int32_t w0 = 0; w0 < P; w0 += nt) {
@@ -236,7 +265,7 @@ __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_ti
             room = most > has ? most - has : 0;
         }
         int64_t all;
-        const int64_t at = given + block_scan64(room, lds.sums, all);
+        const int64_t at = given + block_scan(room, lds.sums, all);
         if (w < P) lds.bound[w] = at < line ? at : line;
         given += all;
     }
@@ -246,12 +275,12 @@ __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_ti
     for (int32_t t0 = 0; t0 < n_tiles; t0 += nt) {
         const int32_t t = t0 + tid;
         if (t >= n_tiles) continue;
-        const RowTile x = tiles[t];
+        const RowTile x = tile_at(t);
         const int64_t end = x.cost0 + tile_cost(x);
         if (x.cost0 < 0 || end == x.cost0) continue;
         for (int32_t w = bound_of(lds.bound, P, x.cost0, true); w < P && lds.bound[w] < end; ++w) {
-            if (lds.bound[w] - x.cost0 <= kTileCost + 2 * kPageCost) lds.bound[w] = x.cost0;
-            else if (end - lds.bound[w] <= 2 * kPageCost) lds.bound[w] = end;
+            if (lds.bound[w] - x.cost0 <= kTileCost + (2 << kPageShift)) lds.bound[w] = x.cost0;
+            else if (end - lds.bound[w] <= (2 << kPageShift)) lds.bound[w] = end;
         }
     }
     __syncthreads();
@@ -261,7 +290,7 @@ __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_ti
         int64_t need = 0;
         int32_t w0 = 0, n_wg = 0;
         if (t < n_tiles) {
-            const RowTile x = tiles[t];
+            const RowTile x = tile_at(t);
             const int64_t end = x.cost0 + tile_cost(x);
             if (x.cost0 < 0) {
                 n_wg = 1;
@@ -274,7 +303,7 @@ __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_ti
             if (!(a.mode == kCross && n_wg == 1)) need = (int64_t)n_wg * x.rows;
         }
         int64_t all;
-        const int64_t at = block_scan64(need, lds.sums, all);
+        const int64_t at = block_scan(need, lds.sums, all);
         if (t < n_tiles) {
             tiles[t].wg0 = w0;
             tiles[t].n_wg = n_wg;
@@ -290,80 +319,76 @@ __device__ __forceinline__ void share_out(const RowsArgs &a, int h, int32_t n_ti
 __device__ __forceinline__ void plan_prefix(const RowsArgs &a, int h, PlanLds &lds)
 {
     const int tid = threadIdx.x, nt = blockDim.x;
-    const int32_t B = a.batch, G = 1 << a.g_log2, per = kTileRows >> a.g_log2;
+    const int32_t B = a.batch, G = 1 << a.g_log2, per = kTileRows >> a.g_log2;  // a power of two
     RowTile *tiles = plan_part<RowTile>(a, h, a.tile_at);
     int32_t *toks = plan_part<int32_t>(a, h, a.tok_at), *lims = plan_part<int32_t>(a, h, a.lim_at);
     int32_t *map = plan_part<int32_t>(a, h, a.map_at);
     for (int32_t b = tid; b < B; b += nt) {
+        lds.item[b] = int2{a.of[b], a.count[b]};
         lds.order[b] = (quantised_end(a, b) - a.s_sink) / kPage;  // complete pages
         lds.most[b] = 0;
+        lds.flag[b] = 0;
     }
+    if (tid == 0) lds.count = 0;
     __syncthreads();
     for (int32_t b = tid; b < B; b += nt) {
-        const int32_t l = a.of[b];
+        const int32_t l = lds.item[b].x;
         int32_t s = 0;
-        if (l >= 0 && l < B && l != b) s = max(min(min(a.count[b], a.max_pages), min(lds.order[b], lds.order[l])), 0);
-        lds.group[b] = s > 0 ? l : -1;
-        lds.len[b] = s;
+        if (l >= 0 && l < B && l != b) s = max(min(min(lds.item[b].y, a.max_pages), min(lds.order[b], lds.order[l])), 0);
+        lds.item[b] = int2{s > 0 ? l : -1, s};
         if (s > 0) atomicMax(&lds.most[l], s);
     }
     __syncthreads();
     for (int32_t b = tid; b < B; b += nt) {
-        if (lds.group[b] < 0 && lds.most[b] > 0) {  // a leader goes with its sequences
-            lds.group[b] = b;
-            lds.len[b] = lds.most[b];
-        }
-        lds.flag[b] = 0;
+        if (lds.item[b].x < 0 && lds.most[b] > 0) lds.item[b] = int2{b, lds.most[b]};  // a leader goes with its sequences
+        if (lds.item[b].x >= 0) atomicAdd(&lds.count, 1);
     }
     __syncthreads();
     // the sequences by leader, then by pages shared (longest first), then by number
-    int32_t at[(kMaxRowItems + 255) / 256], in_group[(kMaxRowItems + 255) / 256];
-    int k = 0;
-    for (int32_t b = tid; b < B; b += nt, ++k) {
-        at[k] = in_group[k] = 0;
-        const int32_t g = lds.group[b], s = lds.len[b];
-        if (g < 0) continue;
-        for (int32_t c = 0; c < B; ++c) {
-            const int32_t gc = lds.group[c], sc = lds.len[c];
-            const bool mate = gc == g && (sc > s || (sc == s && c < b));
-            at[k] += (gc >= 0 && gc < g) || mate;
-            in_group[k] += mate;
+    const int32_t n_sorted = lds.count;
+    for (int32_t b = tid >> 6; b < B; b += nt >> 6) {  // (a wave compares it with 64 at a time)
+        const int2 x = lds.item[b];
+        if (x.x < 0) continue;
+        int32_t before = 0, mates = 0;
+        for (int32_t c0 = 0; c0 < B; c0 += 64) {
+            const int32_t c = c0 + (tid & 63);
+            const int2 y = c < B ? lds.item[c] : int2{-1, 0};
+            mates += __popcll(__ballot(y.x == x.x && (y.y > x.y || (y.y == x.y && c < b))));
+            before += __popcll(__ballot((uint32_t)y.x < (uint32_t)x.x));  // (not those of none)
         }
-        lds.flag[at[k]] = in_group[k] % per == 0;
+        if ((tid & 63) == 0) {
+            lds.order[before + mates] = b;
+            lds.flag[before + mates] = (mates & (per - 1)) == 0;
+        }
     }
     __syncthreads();
-    k = 0;
-    for (int32_t b = tid; b < B; b += nt, ++k)
-        if (lds.group[b] >= 0) lds.order[at[k]] = b;
-    __syncthreads();
     // tiles in that order, behind the sequences' own
-    int32_t n_tiles = B, n_sorted = 0;
-    for (int32_t b = 0; b < B; ++b) n_sorted += lds.group[b] >= 0;
-    for (int32_t p0 = 0; p0 < B; p0 += nt) {
+    int32_t n_tiles = B;
+    for (int32_t p0 = 0; p0 < n_sorted; p0 += nt) {
         const int32_t p = p0 + tid;
         const bool start = p < n_sorted && lds.flag[p] != 0;
         int64_t all;
-        const int32_t before = (int32_t)block_scan64(start, lds.sums, all);
+        const int32_t before = (int32_t)block_scan(start, lds.sums, all);
         if (p < n_sorted) {
             const int32_t b = lds.order[p], t = n_tiles + before + (start ? 1 : 0) - 1;
             toks[B + p] = b;
-            lims[B + p] = lds.len[b];
+            lims[B + p] = lds.item[b].y;
             map[2 * b] = t;
             lds.most[p] = t;  // (the counts it held are used)
             if (start) {
                 int32_t n = 1;
                 while (n < per && p + n < n_sorted && lds.flag[p + n] == 0) ++n;
-                tiles[t] = RowTile{lds.group[b], 0, lds.len[b], 0, n * G, B + p, lds.len[lds.order[p + n - 1]], -1, 0, 0, 0};
+                tiles[t] = RowTile{lds.item[b].x, 0, lds.item[b].y, 0, n * G, B + p, lds.item[lds.order[p + n - 1]].y, -1, 0, 0, 0};
             }
         }
         n_tiles += (int32_t)all;
     }
     for (int32_t b = tid; b < B; b += nt) {
-        const int32_t S = a.seq_len[b], s = lds.len[b];
+        const int32_t S = a.seq_len[b], s = lds.item[b].y;
         const int32_t pages = min((quantised_end(a, b) - a.s_sink + kPage - 1) / kPage, a.max_pages);
         tiles[b] = RowTile{b, s, max(pages - s, 0), S > 0 ? a.win_slots / kPage : 0, G, b, INT32_MAX, -1, 0, 0, 0};
         toks[b] = b;
-        if (lds.group[b] < 0) map[2 * b] = -1;
+        if (lds.item[b].x < 0) map[2 * b] = -1;
     }
     __syncthreads();
     // each sorted sequence's place in its tile
@@ -387,49 +412,53 @@ __device__ __forceinline__ void plan_cross(const RowsArgs &a, int h, PlanLds &ld
     int32_t *toks = plan_part<int32_t>(a, h, a.tok_at);
     for (int32_t i = tid; i < N; i += nt) {
         int32_t src;
-        lds.len[i] = item_tokens(a, i, src);
-        lds.group[i] = lds.len[i] > 0 ? src : -1;
+        const int32_t n = item_tokens(a, i, src);
+        lds.item[i] = int2{n > 0 ? src : -1, n};
     }
+    if (tid == 0) lds.count = 0;
     __syncthreads();
     // the token list goes by stored sequence, then by query sequence
-    int32_t start[(kMaxRowItems + 255) / 256], all_of[(kMaxRowItems + 255) / 256];
-    int k = 0;
-    for (int32_t i = tid; i < N; i += nt, ++k) {
-        const int32_t g = lds.group[i];
-        int32_t at = 0, first = 0, sum = 0;
-        for (int32_t c = 0; g >= 0 && c < N; ++c) {
-            const int32_t gc = lds.group[c], n = lds.len[c];
-            if (gc < 0) continue;
-            if (gc < g) first += n;
-            if (gc == g) sum += n;
-            if (gc < g || (gc == g && c < i)) at += n;
+    // (a wave compares it with 64 at a time; the sums are below 2^24, exact in fp32)
+    for (int32_t i = tid >> 6; i < N; i += nt >> 6) {
+        const int2 x = lds.item[i];
+        float before = 0.0f, first = 0.0f, sum = 0.0f;  // first: of the stored sequences before; before: of the same one's items
+        for (int32_t c = tid & 63; c < N; c += 64) {
+            const int2 y = lds.item[c];  // (those of none have no tokens)
+            const float n = (float)y.y;
+            first += y.x < x.x ? n : 0.0f;
+            sum += y.x == x.x ? n : 0.0f;
+            before += y.x == x.x && c < i ? n : 0.0f;
         }
-        lds.order[i] = at;
-        lds.most[i] = g >= 0 && at == first ? (sum + per - 1) / per : 0;  // tiles, at a stored sequence's first
-        start[k] = first;
-        all_of[k] = sum;
+        const int32_t f = (int32_t)wave_sum(first), t = (int32_t)wave_sum(sum), e = (int32_t)wave_sum(before);
+        if ((tid & 63) == 0) {
+            const int32_t n = x.y > 0 && e == 0 ? (t + per - 1) >> (kTileLog2 - a.g_log2) : 0;  // tiles, at a stored sequence's first
+            lds.order[i] = f + e;
+            lds.most[i] = n;
+            lds.at[i] = f;
+            lds.sum[i] = t;
+            atomicAdd(&lds.count, n);
+        }
     }
     __syncthreads();
-    k = 0;
-    for (int32_t i = tid; i < N; i += nt, ++k) {
-        int32_t before = 0;
-        for (int32_t c = 0; lds.most[i] > 0 && c < N; ++c)
-            if (lds.most[c] > 0 && lds.group[c] < lds.group[i]) before += lds.most[c];
-        lds.flag[i] = before;
+    for (int32_t i = tid >> 6; i < N; i += nt >> 6) {
+        const int32_t g = lds.item[i].x;
+        float before = 0.0f;
+        for (int32_t c = tid & 63; c < N; c += 64) before += lds.item[c].x < g ? (float)lds.most[c] : 0.0f;
+        const int32_t f = (int32_t)wave_sum(before);
+        if ((tid & 63) == 0) lds.flag[i] = f;
     }
-    int32_t n_tiles = 0;
-    for (int32_t c = 0; c < N; ++c) n_tiles += lds.most[c];
-    k = 0;
-    for (int32_t i = tid; i < N; i += nt, ++k) {
-        const int32_t b = lds.group[i];
+    __syncthreads();
+    const int32_t n_tiles = lds.count;
+    for (int32_t i = tid >> 6; i < N; i += nt >> 6) {
+        const int32_t b = lds.item[i].x;
         if (lds.most[i] == 0) continue;
         const int32_t pages = min((quantised_end(a, b) - a.s_sink + kPage - 1) / kPage, a.max_pages);
-        for (int32_t x = 0; x < lds.most[i]; ++x)
-            tiles[lds.flag[i] + x] = RowTile{b, 0, pages, a.win_slots / kPage, min(per, all_of[k] - x * per) * G,
-                                             start[k] + x * per, INT32_MAX, -1, 0, 0, 0};
+        for (int32_t x = tid & 63; x < lds.most[i]; x += 64)
+            tiles[lds.flag[i] + x] = RowTile{b, 0, pages, a.win_slots / kPage, min(per, lds.sum[i] - x * per) * G,
+                                             lds.at[i] + x * per, INT32_MAX, -1, 0, 0, 0};
     }
     for (int32_t i = tid >> 6; i < N; i += nt >> 6)
-        for (int32_t t = tid & 63; t < lds.len[i]; t += 64) toks[lds.order[i] + t] = i * a.max_tok + t;
+        for (int32_t t = tid & 63; t < lds.item[i].y; t += 64) toks[lds.order[i] + t] = i * a.max_tok + t;
     share_out(a, h, n_tiles, lds);
 }
 
@@ -454,8 +483,10 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
 {
     constexpr int R = 16, NT = 64 * kQtWaves<D>;
     using Q = QueryLds<D, R>;
-    constexpr int kBytes = Q::kBytes > (int)sizeof(PlanLds) ? Q::kBytes : (int)sizeof(PlanLds);
+    constexpr int kRaw = (Q::kBytes + 15) / 16 * 16, kRows = kRaw + kReps * R * Q::kQPitch * 2;
+    constexpr int kBytes = kRows > (int)sizeof(PlanLds) ? kRows : (int)sizeof(PlanLds);
     __shared__ __attribute__((aligned(16))) uint8_t lds[kBytes];
+    uint16_t *raw = reinterpret_cast<uint16_t *>(lds + kRaw);
     const int tid = threadIdx.x, h = blockIdx.x;
     if (blockIdx.y == 0) {
         PlanLds &p = *reinterpret_cast<PlanLds *>(lds);
@@ -468,32 +499,45 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
     const int64_t rows = (int64_t)a.items * a.max_tok * G;  // of a kv head
     TColumns<D> tc;
     tc.load(a.tinv, h, tid);
+    // all groups' queries first (in a loop their loads would wait for the stores of the
+    // group before them); rows of no token get zeros
+    const int pr = tid / (D / 8), pc = 8 * (tid % (D / 8));
+    const int64_t first = (int64_t)(blockIdx.y - 1) * a.reps * R;
+    if (tid < R * D / 8) {
+        u32x4 x[kReps];
+        bool there[kReps];
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) {
+            const int64_t row = min(first + k * R + pr, rows - 1);
+            const int32_t tok = (int32_t)(row >> a.g_log2), g = (int32_t)row & (G - 1);
+            x[k] = *reinterpret_cast<const u32x4 *>(a.q + (((int64_t)tok * a.n_kv + h) * G + g) * D + pc);
+            there[k] = true;
+            if (a.mode == kCross) {
+                int32_t src;
+                const uint32_t item = (uint32_t)tok / (uint32_t)a.max_tok;
+                there[k] = tok - (int32_t)item * a.max_tok < item_tokens(a, (int32_t)item, src);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) {
+            const int64_t row = first + k * R + pr;
+            if (k < a.reps && row < rows && !there[k]) {
+                float *to = a.out + (((row >> a.g_log2) * a.n_kv + h) * G + (row & (G - 1))) * D + pc;
+                reinterpret_cast<f32x4 *>(to)[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+                reinterpret_cast<f32x4 *>(to)[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            if (!there[k] || row >= rows) x[k] = u32x4{0u, 0u, 0u, 0u};
+            *reinterpret_cast<u32x4 *>(raw + (k * R + pr) * Q::kQPitch + pc) = x[k];
+        }
+    }
     for (int rep = 0; rep < a.reps; ++rep) {
-        const int64_t row0 = ((int64_t)(blockIdx.y - 1) * a.reps + rep) * R;
+        const int64_t row0 = first + rep * R;
         if (row0 >= rows) return;
         const int n = (int)(rows - row0 < R ? rows - row0 : R);
-        uint16_t *qs = reinterpret_cast<uint16_t *>(lds);
         __syncthreads();
-        for (int i = tid; i < R * D / 8; i += NT) {
-            const int r = i / (D / 8), c = 8 * (i % (D / 8));
-            u32x4 x = {0u, 0u, 0u, 0u};
-            if (r < n) {
-                const int64_t tok = (row0 + r) >> a.g_log2;
-                const int32_t g = (int32_t)(row0 + r) & (G - 1);
-                const int64_t at = ((tok * a.n_kv + h) * G + g) * D + c;
-                int32_t src;
-                // (rows of no token: zeros out)
-                const bool there = a.mode != kCross ||
-                                   tok % a.max_tok < item_tokens(a, (int32_t)(tok / a.max_tok), src);
-                if (there) {
-                    x = *reinterpret_cast<const u32x4 *>(a.q + at);
-                } else {
-                    *reinterpret_cast<f32x4 *>(a.out + at) = f32x4{0.f, 0.f, 0.f, 0.f};
-                    *reinterpret_cast<f32x4 *>(a.out + at + 4) = f32x4{0.f, 0.f, 0.f, 0.f};
-                }
-            }
-            *reinterpret_cast<u32x4 *>(qs + r * Q::kQPitch + c) = x;
-        }
+        if (tid < R * D / 8)
+            *reinterpret_cast<u32x4 *>(reinterpret_cast<uint16_t *>(lds) + pr * Q::kQPitch + pc) =
+                *reinterpret_cast<const u32x4 *>(raw + (rep * R + pr) * Q::kQPitch + pc);
         form_qt_mfma<D, R>(a.scale, tc, lds, tid);
         const int64_t to = (int64_t)h * rows + row0;
         const float *qt = reinterpret_cast<const float *>(lds);
@@ -513,8 +557,11 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
             }
         }
         form_limbs<D, BITS, R, kQtWaves<D>>(lds, tid);
-        for (int i = tid; i < n * kLimbRoom * 128 / 16; i += NT)
-            reinterpret_cast<u32x4 *>(a.qlimb + to * kLimbRoom * 128)[i] = reinterpret_cast<const u32x4 *>(lds)[i];
+        constexpr int kRoom = kLimbRoom * 8, kUsed = Limbs<BITS>::kCount * 8;  // in 16 bytes
+        for (int i = tid; i < n * kUsed; i += NT) {
+            const int at = i / kUsed * kRoom + i % kUsed;
+            reinterpret_cast<u32x4 *>(a.qlimb + to * kLimbRoom * 128)[at] = reinterpret_cast<const u32x4 *>(lds)[at];
+        }
         if (tid < n * 4) a.qaux[to * 4 + tid] = reinterpret_cast<const uint32_t *>(lds + Q::kAux)[tid];
     }
 }
@@ -629,7 +676,7 @@ __device__ __forceinline__ void raise_references(RowState<D> &s, f32x4 (&x)[4], 
 
 template <int D, int BITS, bool WEIGH>
 __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile, int32_t lo, int32_t hi, int32_t slot,
-                                          uint8_t *lds, int h)
+                                          uint8_t *lds, int h, bool late)
 {
     using L = Layout<D, BITS>;
     using LB = Limbs<BITS>;
@@ -744,7 +791,13 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 pg.load_params(p, n);
                 pg.load_values(p, lane);
             }
-            for (; todo != 0;) {
+            // Of two workgroups of a compute unit the older one's waves go first and end
+            // long before the other's (70 against 97 us at 64 sequences on 32K tokens): the
+            // younger goes first through most of a run (the kernel: 100 -> 94 us).
+            if (late) __builtin_amdgcn_s_setprio(1);
+            const int until = __popcll(todo) * 2 / 3;
+            for (int done = 0; todo != 0; ++done) {
+                if (done == until) __builtin_amdgcn_s_setprio(0);
                 todo &= todo - 1;
                 const int next = todo != 0 ? __builtin_ctzll(todo) : cur;
                 const uint8_t *np = page_at(next);
@@ -1058,8 +1111,8 @@ __global__ void __launch_bounds__(256, kRowsPerCu) rows_kernel(RowsArgs a)
     const RowTile *tiles = plan_part<const RowTile>(a, h, a.tile_at);
     // its small tiles (latencies, mostly) and its part of the line, every other
     // workgroup of a compute unit the other way round
-    int32_t s = (int32_t)(((int64_t)w * plan.n_small + a.wgs - 1) / a.wgs);
-    const int32_t s1 = (int32_t)(((int64_t)(w + 1) * plan.n_small + a.wgs - 1) / a.wgs);
+    int32_t s = small_of(a, w, plan.n_small);
+    const int32_t s1 = small_of(a, w + 1, plan.n_small);
     int32_t t = begin < plan.total ? plan_part<const int32_t>(a, h, a.wg_at)[w] : plan.n_tiles;
     const bool late = ((h + a.n_kv * w) / a.cus) & 1;
     for (;;) {
@@ -1084,7 +1137,7 @@ __global__ void __launch_bounds__(256, kRowsPerCu) rows_kernel(RowsArgs a)
         } else {
             break;
         }
-        take_tile<D, BITS, WEIGH>(a, tile, lo, hi, slot, lds, h);
+        take_tile<D, BITS, WEIGH>(a, tile, lo, hi, slot, lds, h, late);
     }
 }
 
@@ -1182,8 +1235,8 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a)
     }
 }
 
-// Cross: workgroup w merges the tile that workgroup w of rows_kernel began and did
-// not end.
+// Cross: workgroups (h, w, ..) merge the tile that workgroup w of rows_kernel began and
+// did not end, a wave a row.
 template <int D>
 __global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a)
 {
@@ -1194,7 +1247,8 @@ __global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a)
     const RowTile tile = plan_part<const RowTile>(a, h, a.tile_at)[plan_part<const int32_t>(a, h, a.wg_at)[w + 1]];
     if (tile.cost0 == at || tile.wg0 != w) return;
     const int32_t *toks = plan_part<const int32_t>(a, h, a.tok_at) + tile.tok;
-    for (int r = wave; r < tile.rows; r += 4) {
+    const int r = 4 * blockIdx.z + wave;
+    if (r < tile.rows) {
         float o[D / 64], M, l;
         merge_row<D>(a, h, tile.n_wg, [&](int i) -> int64_t { return tile.part + (int64_t)i * tile.rows + r; }, o, M, l);
         const int64_t to = (((int64_t)toks[r >> a.g_log2] * a.n_kv + h) << a.g_log2) + (r & (G - 1));
@@ -1240,6 +1294,7 @@ static int64_t lay_out(const wushkv_cache *c, int32_t mode, int32_t n_q, int64_t
     };
     a.cus = (int32_t)compute_units();
     a.wgs = (int32_t)std::min<int64_t>(std::max<int64_t>(kRowsPerCu * compute_units() / hk, 1), kMaxWgs);
+    a.inverse = a.wgs > 1 ? UINT64_MAX / (uint64_t)a.wgs + 1 : UINT64_MAX;
     // (cross: a stored sequence's last tile may be short)
     const int64_t tiles = mode == kPrefix ? 2 * B : mode == kWeighted ? B : (tokens * G + kTileRows - 1) / kTileRows + (items < B ? items : B);
     a.part_rows = mode == kPrefix ? 2 * B * G + kTileRows * (int64_t)a.wgs
@@ -1289,7 +1344,7 @@ static void launch_rows(const RowsArgs &a, hipStream_t s)
     if (a.mode == kWeighted) launch("rows_kernel", rows_kernel<D, BITS, true>, gm, dim3(256), s, a);
     else launch("rows_kernel", rows_kernel<D, BITS, false>, gm, dim3(256), s, a);
     if (a.mode != kCross) launch("rows_merge_kernel", rows_merge_kernel<D>, dim3(a.n_kv, a.batch), dim3(256), s, a);
-    else if (a.wgs > 1) launch("rows_join_kernel", rows_join_kernel<D>, dim3(a.n_kv, a.wgs - 1), dim3(256), s, a);
+    else if (a.wgs > 1) launch("rows_join_kernel", rows_join_kernel<D>, dim3(a.n_kv, a.wgs - 1, kTileRows / 4), dim3(256), s, a);
 }
 
 static int attend_rows(const wushkv_cache *c, RowsArgs &a, int32_t n_q, int64_t max_sel, float sm_scale, void *workspace,
@@ -1318,7 +1373,7 @@ static int attend_rows(const wushkv_cache *c, RowsArgs &a, int32_t n_q, int64_t 
     a.mid = 0.5f * ((1 << c->bits) - 1);
     const int64_t groups = (((int64_t)a.items * a.max_tok << a.g_log2) + 15) / 16;
     a.reps = 1;
-    while (a.reps < 8 && groups * a.n_kv / (2 * a.reps) >= 2 * compute_units()) a.reps *= 2;
+    while (a.reps < kReps && groups * a.n_kv / (2 * a.reps) >= 2 * compute_units()) a.reps *= 2;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     switch (c->head_dim * 10 + storage_bits(c->bits)) {
         case 1282: launch_rows<128, 2>(a, s); break;
