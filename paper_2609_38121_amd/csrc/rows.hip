@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
 // scale the largest (fp16 holds nothing below 2^-24, where the lo parts of small
 // weights would be lost), and at most 2^(kGrow + 1) later.  A window's reference lies
 // 2^kRoom above the maximum, so that sums of values near bf16's largest stay finite.
-constexpr float kLift = 4.0f, kGrow = 14.0f, kRoom = 12.0f;
+constexpr float kLift = 8.0f, kGrow = 14.0f, kRoom = 12.0f;
 // Rows of weights in LDS: 64 tokens of two bytes, and room that spreads the rows read
 // together over the banks.
 constexpr int kPitch = 144;
