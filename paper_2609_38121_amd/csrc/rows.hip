@@ -6,10 +6,9 @@
 //   wushkv_weighted_attention  decode queries, adding up what each page received
 //
 // Launches on the caller's stream:
-//   rows_query_kernel  q~ = q T_K^{-1} of 16 rows at a time with its digit limbs
-//                      (for the pages) and three bf16 parts (for the windows); and,
-//                      in a workgroup per kv head, the plan: tiles and how they are
-//                      shared out (below).
+//   rows_query_kernel  q~ = q T_K^{-1} of 16 rows at a time (fp32, for the windows)
+//                      and its digit limbs (for the pages); and, in a workgroup per
+//                      kv head, the plan: tiles and how they are shared out (below).
 //   rows_kernel        one residency round of workgroups over the plan.
 //   rows_merge_kernel / rows_join_kernel   what several workgroups have of a row,
 //                      merged; the pages' weights.
@@ -30,14 +29,23 @@
 // limb; keys are centred (k = s (c - mid) + (z + mid s)).  A wave reads a page's
 // codes and parameters from memory in operand order into registers, the next page's
 // while it computes.  Lane (j, n) has rows 4 j + r of tokens 4 n + t.  A row's
-// softmax has a reference that stays kLift below its maximum at the time and moves
-// only when a weight would pass 2^kGrow, so that a page costs one test.  Weights
+// softmax has a reference, a whole number, at its maximum of the time, that moves only
+// when a weight would pass 2^kGrow, so that a page costs one test.  Weights
 // p s go through LDS as fp16 hi + lo parts, each formed from the exact product, to
 // be the rows of the P V products with the value codes as fp16 numbers 16 c.  The
 // value scales are brought to about one by a power of two that the wave keeps
 // (tiny scales would leave the lo parts no bits); sums of p z and p are fp32.
 //
 // Windows.  q~ and weights in three bf16 parts, 64 slots at a time.
+//
+// What bounds it.  A page of 16 rows is about 415 vector instructions (144 of them the
+// widening of its 8192 value codes), 20 scaled products and 32 fp16 ones, all issued from
+// one port; two workgroups a compute unit keep the vector units 62 to 69% busy.  64
+// sequences on 32768 tokens (d 128, 2-bit, 8 kv heads, G 4): rows_kernel 95 us for 65536
+// page passes, 0.8 us each on a SIMD; 8 sequences of 256 tokens over up to 4000: 175 us;
+// 64 x 16-32K tokens weighted, 128 pages of each: 57 us, 3.5 TB/s of pages.  Tiles of 32
+// rows would halve the widening, but at two workgroups a compute unit their registers
+// spill (116 us in the first case), and three workgroups spill with 16 rows.
 #include <algorithm>
 #include <atomic>
 
@@ -48,7 +56,7 @@ namespace wushkv {
 constexpr int kMaxRowItems = 1024;  // sequences that a plan sorts
 constexpr int kMaxWgs = 1024;       // workgroups of rows_kernel per kv head
 constexpr int kTileLog2 = 4, kTileRows = 1 << kTileLog2;
-constexpr int kReps = 4;        // most 16-row groups that a workgroup of rows_query_kernel takes
+constexpr int kReps = 2;        // most 16-row groups that a workgroup of rows_query_kernel takes
 constexpr int kRowsPerCu = 2;  // workgroups of rows_kernel that a compute unit keeps
 
 // Tiles of one stored sequence's pages for up to 16 query rows.
@@ -92,7 +100,7 @@ struct RowsArgs {
     // workspace
     uint8_t *qlimb;               // [n_kv][tokens][G][6][128]
     uint32_t *qaux;               // [n_kv][tokens][G][4]
-    uint16_t *qpart;              // bf16 [n_kv][tokens][G][3][D]
+    float *qt;                    // [n_kv][tokens][G][D]: q~
     uint8_t *plan;                // per kv head plan_bytes
     int64_t plan_bytes;
     // offsets in a plan: int64 [wgs + 1], where the workgroups' parts of the line begin;
@@ -478,6 +486,68 @@ __device__ __forceinline__ void plan_weighted(const RowsArgs &a, int h, PlanLds 
 
 // ------------------------------------------------------------------ q~
 
+// The digit limbs of form_limbs, for 16 rows at once: a thread has channels c .. c + 3
+// of its row, D / 4 neighbours the row.  (Two rows a wave instead of one, the digits of
+// N from one sum with all of them moved to 0 .. base - 1, six-bit codes packed between
+// neighbours: rows_query_kernel takes 52.8 instead of 55.4 us for 65536 rows.)  Returns the
+// limbs' scales; out: the row's limbs.
+template <int D, int BITS>
+__device__ __forceinline__ u32x2 row_limbs(const f32x4 &x, uint8_t *out, int c)
+{
+    using LB = Limbs<BITS>;
+    float mx = row_max16(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))));
+    if constexpr (D == 128) mx = fmaxf(mx, __shfl_xor(mx, 16));
+    int F = 0;
+    if (mx > 0.0f) {
+        int ex;
+        (void)frexpf(LB::kNMax / mx, &ex);
+        F = ex - 1;
+        if (ldexpf(mx, F) > LB::kNMax) F -= 1;
+        if (ldexpf(mx, F + 1) <= LB::kNMax) F += 1;
+        F = F < -100 ? -100 : (F > 100 ? 100 : F);
+    }
+    u32x2 scales = {0u, 0u};
+#pragma unroll
+    for (int l = 0; l < LB::kCount; ++l)
+        scales[l >> 2] |= (uint32_t)(127 + LB::kUnit + LB::kDigitBits * (LB::kCount - 1 - l) - F) << (8 * (l & 3));
+    constexpr int kHalf = 1 << (LB::kDigitBits - 1);
+    constexpr int all_halves = [] {
+        int v = 0;
+        for (int l = 0; l < LB::kCount; ++l) v = (v << LB::kDigitBits) + (1 << (LB::kDigitBits - 1));
+        return v;
+    }();
+    uint32_t N[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) N[e] = (uint32_t)((int)rintf(ldexpf(x[e], F))) + (uint32_t)all_halves;
+    const int q = (c >> 2) & 3;
+#pragma unroll
+    for (int l = 0; l < LB::kCount; ++l) {
+        int d[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            d[e] = (int)((N[e] >> (LB::kDigitBits * (LB::kCount - 1 - l))) & (2 * kHalf - 1)) - kHalf;
+        if constexpr (BITS == 2) {
+            // fp6 e2m3 of d / 8: sign and integer; 16 channels are three words
+            uint32_t p = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p |= ((uint32_t)max(d[e], -d[e]) | ((uint32_t)(d[e] >> 26) & 0x20u)) << (6 * e);
+            const uint32_t above = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)p, 0xF9, 0xF, 0xF, true);  // the next thread's
+            if (q < 3)
+                *reinterpret_cast<uint32_t *>(out + l * 128 + 32 * (c >> 5) + 12 * ((c >> 4) & 1) + 4 * q) =
+                    (p >> (8 * q)) | (above << (24 - 8 * q));
+        } else {
+            // fp8 e4m3 of d, exact
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32((float)d[0], (float)d[1], 0, false);
+            w = __builtin_amdgcn_cvt_pk_fp8_f32((float)d[2], (float)d[3], w, true);
+            *reinterpret_cast<int *>(out + l * 128 + c) = w;
+        }
+        if constexpr (D == 64) {  // channels 64 .. 127 of the operands: none
+            *reinterpret_cast<uint32_t *>(out + l * 128 + 64 + c) = 0u;
+        }
+    }
+    return scales;
+}
+
 template <int D, int BITS>
 __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a)
 {
@@ -530,6 +600,8 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
             *reinterpret_cast<u32x4 *>(raw + (k * R + pr) * Q::kQPitch + pc) = x[k];
         }
     }
+    static_assert(NT == R * D / 4, "a thread has four channels of a row");
+    const int r = tid / (D / 4), c = 4 * (tid % (D / 4));
     for (int rep = 0; rep < a.reps; ++rep) {
         const int64_t row0 = first + rep * R;
         if (row0 >= rows) return;
@@ -540,29 +612,17 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
                 *reinterpret_cast<const u32x4 *>(raw + (rep * R + pr) * Q::kQPitch + pc);
         form_qt_mfma<D, R>(a.scale, tc, lds, tid);
         const int64_t to = (int64_t)h * rows + row0;
-        const float *qt = reinterpret_cast<const float *>(lds);
-        for (int i = tid; i < n * D / 4; i += NT) {
-            const int r = i / (D / 4), c = 4 * (i % (D / 4));
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(qt + r * D + c);
-            float e[4] = {x[0], x[1], x[2], x[3]};
-            uint16_t *dst = a.qpart + (to + r) * 3 * D + c;
-#pragma unroll
-            for (int part = 0; part < 3; ++part) {
-                const uint32_t u0 = pack_bf16_rne(e[0], e[1]), u1 = pack_bf16_rne(e[2], e[3]);
-                *reinterpret_cast<uint2 *>(dst + part * D) = uint2{u0, u1};
-                e[0] -= bf16_bits_to_f32(u0 & 0xFFFFu);
-                e[1] -= bf16_bits_to_f32(u0 >> 16);
-                e[2] -= bf16_bits_to_f32(u1 & 0xFFFFu);
-                e[3] -= bf16_bits_to_f32(u1 >> 16);
-            }
-        }
-        form_limbs<D, BITS, R, kQtWaves<D>>(lds, tid);
+        const f32x4 x = reinterpret_cast<const f32x4 *>(lds)[tid];
+        __syncthreads();  // (read: the limbs go there)
+        if (r < n) *reinterpret_cast<f32x4 *>(a.qt + (to + r) * D + c) = x;
+        const u32x2 scales = row_limbs<D, BITS>(x, lds + r * kLimbRoom * 128, c);
+        if (r < n && c == 0) *reinterpret_cast<u32x2 *>(a.qaux + (to + r) * 4) = scales;
+        __syncthreads();
         constexpr int kRoom = kLimbRoom * 8, kUsed = Limbs<BITS>::kCount * 8;  // in 16 bytes
         for (int i = tid; i < n * kUsed; i += NT) {
             const int at = i / kUsed * kRoom + i % kUsed;
             reinterpret_cast<u32x4 *>(a.qlimb + to * kLimbRoom * 128)[at] = reinterpret_cast<const u32x4 *>(lds)[at];
         }
-        if (tid < n * 4) a.qaux[to * 4 + tid] = reinterpret_cast<const uint32_t *>(lds + Q::kAux)[tid];
     }
 }
 
@@ -570,9 +630,12 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
 
 // A page's weight p s is about 2^kLift where a row's maximum is new and the value
 // scale the largest (fp16 holds nothing below 2^-24, where the lo parts of small
-// weights would be lost), and at most 2^(kGrow + 1) later.  A window's reference lies
-// 2^kRoom above the maximum, so that sums of values near bf16's largest stay finite.
-constexpr float kLift = 8.0f, kGrow = 14.0f, kRoom = 12.0f;
+// weights would be lost), and at most 2^(kLift + kGrow + 1) later.  A window's weights
+// are taken times 2^-kRoom, so that sums of values near bf16's largest stay finite.
+// Both go by factors of the values, not by the logits: an exponential's argument near
+// zero has the smaller rounding (one token's row of 700: 6e-7 with references 8 below
+// the maximum, up to 1.9e-6 of its norm).
+constexpr float kLift = 6.0f, kGrow = 8.0f, kRoom = 12.0f;
 // Rows of weights in LDS: 64 tokens of two bytes, and room that spreads the rows read
 // together over the banks.
 constexpr int kPitch = 144;
@@ -653,14 +716,17 @@ __device__ __forceinline__ void move_references(RowState<D> &s, const f32x4 &up)
     for (int nt = 0; nt < D / 16; ++nt) s.acc[nt] *= f;
 }
 
-// Moves the references of logits x, relative to them, so that a row's largest is at
-// most lift.  A row that sees none of the first tokens stays: it sees none later either.
+// Moves the references of logits x, relative to them, to the whole number at or above a
+// row's largest (whole, so that what is brought from one reference to another is brought
+// by a power of two).  A row that sees none of the first tokens stays: it sees none later
+// either.
 template <int D>
-__device__ __forceinline__ void raise_references(RowState<D> &s, f32x4 (&x)[4], float lift, bool fresh)
+__device__ __forceinline__ void raise_references(RowState<D> &s, f32x4 (&x)[4], bool fresh)
 {
     f32x4 up;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) up[r] = row_max16(fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[2][r], x[3][r]))) - lift;
+    for (int r = 0; r < 4; ++r)
+        up[r] = ceilf(row_max16(fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[2][r], x[3][r]))));
     if (fresh) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) up[r] = up[r] == -INFINITY ? 0.0f : up[r];
@@ -707,6 +773,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
     s.m = s.l = s.z = f32x4{0.f, 0.f, 0.f, 0.f};
     bool fresh = true;  // nothing seen, references 0
     float unit = 1.0f;  // what acc is counted in
+    float in_room = 1.0f;  // what m, l and z will be, for sums with windows
 
     const int32_t page_hi = min(hi, tile.n_pages);
     if (lo < page_hi) {
@@ -745,13 +812,18 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
             }
         };
+        // c += the products, those of the largest digits apart from the others' sum, which
+        // is rounded far below (every sum onto c would round at its size)
         auto products = [&](const i32x8 (&bop)[4], f32x4 (&c)[4]) {
+            f32x4 rest[4] = {};
+            if constexpr (LB::kCount > 5) limb_products<BITS, 5, kScaleB>(limb(5), bop, (int)sc[1], rest);
+            limb_products<BITS, 4, kScaleB>(limb(4), bop, (int)sc[1], rest);
+            limb_products<BITS, 3, kScaleB>(limb(3), bop, (int)sc[0], rest);
+            limb_products<BITS, 2, kScaleB>(limb(2), bop, (int)sc[0], rest);
+            limb_products<BITS, 1, kScaleB>(limb(1), bop, (int)sc[0], rest);
             limb_products<BITS, 0, kScaleB>(limb(0), bop, (int)sc[0], c);
-            limb_products<BITS, 1, kScaleB>(limb(1), bop, (int)sc[0], c);
-            limb_products<BITS, 2, kScaleB>(limb(2), bop, (int)sc[0], c);
-            limb_products<BITS, 3, kScaleB>(limb(3), bop, (int)sc[0], c);
-            limb_products<BITS, 4, kScaleB>(limb(4), bop, (int)sc[1], c);
-            if constexpr (LB::kCount > 5) limb_products<BITS, 5, kScaleB>(limb(5), bop, (int)sc[1], c);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) c[t] += rest[t];
         };
         // the digit sums, by products with keys of code 1 (every column the same), from
         // which the products start
@@ -769,9 +841,9 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
         // where the lane writes its weights (rows 4 j + r, tokens 4 n ..) and reads the
         // operand of row n (tokens 32 kc + 8 j ..)
         const uint32_t pw = pbuf + 4 * j * kPitch + 8 * n, pr = pbuf + n * kPitch + 16 * j;
-        float grow = kGrow;
-        // value scales up to 2^vex are served: the references lie 2^vex higher
+        // value scales up to 2^vex are served: they are taken times vscale, 2^(kLift - vex)
         int vex = 0;
+        float vscale = 0.0f;
         uint32_t vmost = 0u;    // the largest (fp16 bits)
 
         for (int32_t base = lo; base < page_hi; base += 256) {
@@ -814,12 +886,13 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 if (__any(big > vmost)) {  // the largest scale lies in [2^(ex - 1), 2^ex)
                     int ex;
                     (void)frexpf(fminf(wave_max(f16_bits_to_f32(big)), 65504.0f), &ex);
-                    // (where there was no scale so far, down too)
-                    const float up = vmost == 0u ? -40.0f : (float)max(ex - vex, 0);
-                    if (!fresh) move_references<D>(s, f32x4{up, up, up, up});
-                    vex = ex;
-                    vmost = ex >= 16 ? 0x7FFFu : f32_to_f16_bits(ldexpf(2.0f, ex));  // (and twice that)
-                    grow = kGrow - (float)ex;
+                    if (vmost == 0u) vex = ex;  // (no sums but of zeros)
+                    const float down = ldexpf(1.0f, vex - max(ex, vex));
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) s.acc[nt] *= down;
+                    vex = max(ex, vex);
+                    vmost = vex >= 16 ? 0x7FFFu : f32_to_f16_bits(ldexpf(2.0f, vex));  // (and twice that)
+                    vscale = ldexpf(1.0f, (int)kLift - vex);
                 }
                 i32x8 bop[4];
 #pragma unroll
@@ -868,7 +941,10 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
                     most = fmaxf(fmaxf(most, fmaxf(x[t][0], x[t][1])), fmaxf(x[t][2], x[t][3]));
-                if (fresh || __any(most > grow)) raise_references<D>(s, x, kLift - (float)vex, fresh);
+                if (fresh || __any(most > kGrow)) raise_references<D>(s, x, fresh);
+                float vs[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) vs[t] = fmaf((float)lo16(pg.vp[t]), vscale, 0.0f);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     uint32_t hi2[2], lo2[2];
@@ -882,7 +958,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                     // that the lo parts read them where they are, two to a register)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float s0 = (float)lo16(pg.vp[2 * k]), s1 = (float)lo16(pg.vp[2 * k + 1]);
+                        const float s0 = vs[2 * k], s1 = vs[2 * k + 1];
                         const f16x2 ph = {(_Float16)fmaf(p[2 * k], s0, 0.0f), (_Float16)fmaf(p[2 * k + 1], s1, 0.0f)};
                         hi2[k] = __builtin_bit_cast(uint32_t, ph);
                         asm("" : "+v"(hi2[k]));
@@ -941,7 +1017,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 cur = next;
             }
         }
-        unit = 0.0625f;
+        unit = ldexpf(0.0625f, vex - (int)kLift);
     }
 
     if (hi > tile.n_pages) {
@@ -950,14 +1026,16 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
         j = lane >> 4;
         n = lane & 15;
         const uint32_t pw = pbuf + 4 * j * kPitch + 8 * n, pr = pbuf + n * kPitch + 16 * j;
+        const float room = ldexpf(1.0f, -(int)kRoom);
         const int32_t ring = a.win_slots - a.s_sink;
         const int32_t a0 = S > q_hi ? (q_hi - a.s_sink) % ring : 0;
         const int32_t ring_live = S > q_hi ? S - q_hi : 0;
         const int64_t head = (int64_t)b * a.n_kv + h;
 #pragma unroll
-        for (int nt = 0; nt < kNT; ++nt) s.acc[nt] *= unit;
-        const uint16_t *q = a.qpart + row_at(n) * 3 * D + 8 * j;
+        for (int nt = 0; nt < kNT; ++nt) s.acc[nt] *= unit * room;
+        const float *q = a.qt + row_at(n) * D + 8 * j;
         unit = 1.0f;
+        in_room = room;
         const int32_t from = max(lo, tile.n_pages);
         for (int32_t u = from + ((wave - (from - lo)) & 3); u < hi; u += 4) {
             const int32_t slot0 = kPage * (u - tile.n_pages);
@@ -974,17 +1052,32 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 #pragma unroll
             for (int half = 0; half < kC; half += 2) {
                 bf16x8 kx[2][4], qp[2][3];
+                f32x4 qx[2][2];
 #pragma unroll
                 for (int ch = 0; ch < 2; ++ch) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) qx[ch][i] = *reinterpret_cast<const f32x4 *>(q + 32 * (half + ch) + 4 * i);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
                         kx[ch][t] = *reinterpret_cast<const bf16x8 *>(
                             a.win_k + (head * a.win_slots + slot0 + 4 * n + t) * D + 32 * (half + ch) + 8 * j);
-#pragma unroll
-                    for (int p = 0; p < 3; ++p)
-                        qp[ch][p] = *reinterpret_cast<const bf16x8 *>(q + p * D + 32 * (half + ch));
                 }
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) {
+                        u32x4 w;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            f32x4 &x = qx[ch][i / 2];
+                            const int e = 2 * (i % 2);
+                            w[i] = pack_bf16_rne(x[e], x[e + 1]);
+                            x[e] -= bf16_bits_to_f32(w[i] & 0xFFFFu);
+                            x[e + 1] -= bf16_bits_to_f32(w[i] >> 16);
+                        }
+                        qp[ch][p] = __builtin_bit_cast(bf16x8, w);
+                    }
 #pragma unroll
                 for (int ch = 0; ch < 2; ++ch)
 #pragma unroll
@@ -1010,13 +1103,15 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                     c[t][r] = (seen >> t) & 1u ? c[t][r] - s.m[r] : -INFINITY;
                     most = fmaxf(most, c[t][r]);
                 }
-            if (fresh || __any(most > -kRoom)) raise_references<D>(s, c, -kRoom, fresh);
+            if (fresh || __any(most > 0.0f)) raise_references<D>(s, c, fresh);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float p[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) p[t] = fexp2(c[t][r]);
                 s.l[r] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) p[t] *= room;
 #pragma unroll
                 for (int q = 0; q < 3; ++q) {
                     const uint32_t u0 = pack_bf16_rne(p[0], p[1]), u1 = pack_bf16_rne(p[2], p[3]);
@@ -1058,11 +1153,11 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int row = 4 * j + r;
-        const float z = row_sum16(s.z[r]), l = row_sum16(s.l[r]);
+        const float z = row_sum16(s.z[r]) * in_room, l = row_sum16(s.l[r]) * in_room;
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) o[row][16 * nt + n] = fmaf(s.acc[nt][r], unit, z);
         if (n == 0) {
-            sm[wave * 16 + row] = l == 0.0f ? -INFINITY : s.m[r];  // (none: no token seen)
+            sm[wave * 16 + row] = l == 0.0f ? -INFINITY : in_room < 1.0f ? s.m[r] + kRoom : s.m[r];  // (none: no token seen)
             sl[wave * 16 + row] = l;
         }
     }
@@ -1301,7 +1396,7 @@ static int64_t lay_out(const wushkv_cache *c, int32_t mode, int32_t n_q, int64_t
                   : mode == kWeighted ? B * G + G * (int64_t)a.wgs : 2 * kTileRows * (int64_t)a.wgs;
     a.qlimb = take(hk * tokens * G * kLimbRoom * 128);
     a.qaux = reinterpret_cast<uint32_t *>(take(hk * tokens * G * 16));
-    a.qpart = reinterpret_cast<uint16_t *>(take(hk * tokens * G * 3 * d * 2));
+    a.qt = reinterpret_cast<float *>(take(hk * tokens * G * d * 4));
     a.part = reinterpret_cast<float *>(take(hk * a.part_rows * d * 4));
     a.part_ml = reinterpret_cast<float *>(take(hk * a.part_rows * 8));
     if (mode == kWeighted) a.stat = reinterpret_cast<float *>(take(hk * B * max_sel * G * 8));
@@ -1372,8 +1467,10 @@ static int attend_rows(const wushkv_cache *c, RowsArgs &a, int32_t n_q, int64_t 
     a.scale = sm_scale * kLog2e;
     a.mid = 0.5f * ((1 << c->bits) - 1);
     const int64_t groups = (((int64_t)a.items * a.max_tok << a.g_log2) + 15) / 16;
-    a.reps = 1;
-    while (a.reps < kReps && groups * a.n_kv / (2 * a.reps) >= 2 * compute_units()) a.reps *= 2;
+    // (two where there is more than one round of workgroups: 49.7 us for 65536 rows, 51.3
+    // with up to four, 61.9 with up to eight)
+    const int64_t round = 3 * compute_units();
+    a.reps = (int32_t)std::min<int64_t>((groups * a.n_kv + round - 1) / round, kReps);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     switch (c->head_dim * 10 + storage_bits(c->bits)) {
         case 1282: launch_rows<128, 2>(a, s); break;
