@@ -287,14 +287,25 @@ __device__ __forceinline__ f32x4 mfma_scaled(const i32x8 &a, const i32x8 &b, int
 // 1024 (whose bit 0 is 1) is 1024 + c 2^F, and one fused step takes it to
 // (1024 + c 2^F) 2^(4-F) - 1024 2^(4-F) = 16 c, exactly, from whatever field the
 // page has it in; only fields past the fraction are shifted first.  The
-// constants stay in registers (an instruction takes one that is not).
-template <int BITS>
+// constants stay in registers (an instruction takes one that is not).  With a middle
+// they are 16 (c - MIDDLE), as exactly.
+template <int BITS, int MIDDLE = 0>
 struct WidenNormal {
     uint32_t one;       // 1024, twice
-    f16x2 add[5];       // -1024 2^(4-F), F = 0, 2, 4, 6, 8
+    f16x2 add[5];       // -1024 2^(4-F) - 16 MIDDLE, F = 0, 2, 4, 6, 8
+    // -x in fp16, twice
+    static constexpr uint32_t minus(int x)
+    {
+        int e = 0;
+        while ((2 << e) <= x) ++e;
+        const uint32_t bits = 0x8000u | (uint32_t)(e + 15) << 10 | (uint32_t)(((x << 10) >> e) - 1024);
+        return bits << 16 | bits;
+    }
+    static_assert(MIDDLE < 64, "one binade each");
     __device__ __forceinline__ void init()
     {
-        uint32_t v[6] = {0x64006400u, 0xF400F400u, 0xEC00EC00u, 0xE400E400u, 0xDC00DC00u, 0xD400D400u};
+        uint32_t v[6] = {0x64006400u, minus(16384 + 16 * MIDDLE), minus(4096 + 16 * MIDDLE), minus(1024 + 16 * MIDDLE),
+                         minus(256 + 16 * MIDDLE), minus(64 + 16 * MIDDLE)};
 #pragma unroll
         for (int i = 0; i < 6; ++i) asm volatile("" : "+v"(v[i]));
         one = v[0];

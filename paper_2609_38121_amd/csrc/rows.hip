@@ -32,9 +32,9 @@
 // softmax has a reference, a whole number, at its maximum of the time, that moves only
 // when a weight would pass 2^kGrow, so that a page costs one test.  Weights
 // p s go through LDS as fp16 hi + lo parts, each formed from the exact product, to
-// be the rows of the P V products with the value codes as fp16 numbers 16 c.  The
+// be the rows of the P V products with the value codes as fp16 numbers 16 (c - middle).  The
 // value scales are brought to about one by a power of two that the wave keeps
-// (tiny scales would leave the lo parts no bits); sums of p z and p are fp32.
+// (tiny scales would leave the lo parts no bits); sums of p (z + middle s) and p are fp32.
 //
 // Windows.  q~ and weights in three bf16 parts, 64 slots at a time.
 //
@@ -486,7 +486,19 @@ __device__ __forceinline__ void plan_weighted(const RowsArgs &a, int h, PlanLds 
 
 // ------------------------------------------------------------------ q~
 
-// The digit limbs of form_limbs, for 16 rows at once: a thread has channels c .. c + 3
+// Digit limbs of these rows: six base-32 digits (up to 16, whole numbers of both formats),
+// 30 bits of the row's largest entry.  (decode's 24 or 25 are the larger part of a short
+// sequence's error: 700 tokens, up to 8e-7 of a row's norm where a plain fp32 q~ gives up to
+// 6e-7.  The sixth limb of 2-bit keys costs four of 56 products a page.)
+template <int BITS>
+struct RowLimbs {
+    static constexpr int kCount = 6, kDigitBits = 5;
+    static constexpr int kUnit = Limbs<BITS>::kUnit;
+    static constexpr float kNMax = 519552480.0f;  // 15 (1 + 32 + .. + 32^5), as far as fp32 has it
+};
+static_assert(RowLimbs<2>::kCount <= kLimbRoom, "a row's room");
+
+// The digit limbs as in form_limbs, for 16 rows at once: a thread has channels c .. c + 3
 // of its row, D / 4 neighbours the row.  (Two rows a wave instead of one, the digits of
 // N from one sum with all of them moved to 0 .. base - 1, six-bit codes packed between
 // neighbours: rows_query_kernel takes 52.8 instead of 55.4 us for 65536 rows.)  Returns the
@@ -494,7 +506,7 @@ __device__ __forceinline__ void plan_weighted(const RowsArgs &a, int h, PlanLds 
 template <int D, int BITS>
 __device__ __forceinline__ u32x2 row_limbs(const f32x4 &x, uint8_t *out, int c)
 {
-    using LB = Limbs<BITS>;
+    using LB = RowLimbs<BITS>;
     float mx = row_max16(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))));
     if constexpr (D == 128) mx = fmaxf(mx, __shfl_xor(mx, 16));
     int F = 0;
@@ -618,7 +630,7 @@ __global__ void __launch_bounds__(64 * kQtWaves<D>) rows_query_kernel(RowsArgs a
         const u32x2 scales = row_limbs<D, BITS>(x, lds + r * kLimbRoom * 128, c);
         if (r < n && c == 0) *reinterpret_cast<u32x2 *>(a.qaux + (to + r) * 4) = scales;
         __syncthreads();
-        constexpr int kRoom = kLimbRoom * 8, kUsed = Limbs<BITS>::kCount * 8;  // in 16 bytes
+        constexpr int kRoom = kLimbRoom * 8, kUsed = RowLimbs<BITS>::kCount * 8;  // in 16 bytes
         for (int i = tid; i < n * kUsed; i += NT) {
             const int at = i / kUsed * kRoom + i % kUsed;
             reinterpret_cast<u32x4 *>(a.qlimb + to * kLimbRoom * 128)[at] = reinterpret_cast<const u32x4 *>(lds)[at];
@@ -647,7 +659,7 @@ struct RowsLds {
     static constexpr int most(int a, int b) { return a > b ? a : b; }
     static constexpr int kWave = most(16 * D * 4, 3 * 16 * kPitch);
     static constexpr int kLimb = BITS == 2 ? 64 * 24 : 64 * 32;  // of 16 rows: [lane] 16 bytes, [lane] the rest
-    static constexpr int kMl = 4 * kWave + Limbs<BITS>::kCount * kLimb;  // m, then l: float [4][16] each
+    static constexpr int kMl = 4 * kWave + RowLimbs<BITS>::kCount * kLimb;  // m, then l: float [4][16] each
     static constexpr int kBytes = kMl + 2 * 4 * 16 * 4;
     __host__ __device__ static constexpr int limb_at(int l) { return 4 * kWave + l * kLimb; }
 };
@@ -700,8 +712,8 @@ __device__ __forceinline__ void wave_fence()
 // The running softmax of rows 4 j + r: a weight is 2^(logit - m).
 template <int D>
 struct RowState {
-    f32x4 acc[D / 16];  // sums of p s 16 c (pages) or p v (windows), channels 16 nt + n
-    f32x4 m, l, z;      // reference, sum of p, sum of p z (the lane's tokens)
+    f32x4 acc[D / 16];  // sums of p s 16 (c - middle) (pages) or p v (windows), channels 16 nt + n
+    f32x4 m, l, z;      // reference, sum of p, sum of p (z + middle s) (the lane's tokens)
 };
 
 // Moves the references up, and what is relative to them.
@@ -745,10 +757,12 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                                           uint8_t *lds, int h, bool late)
 {
     using L = Layout<D, BITS>;
-    using LB = Limbs<BITS>;
+    using LB = RowLimbs<BITS>;
     using Lds = RowsLds<D, BITS>;
     constexpr int kNT = L::kNTiles, kC = L::kChunks, kScaleB = BITS == 2 ? 128 : 136;
     constexpr int kPlane = 16 * kPitch;
+    // values as s (c - kMiddle) + (z + kMiddle s): the sums of both are then of the output's size
+    constexpr int kMiddle = BITS == 2 ? 2 : 8;
     // (the lane is opaque where a part begins, so that the addresses that follow from
     // it are formed there, and do not hold registers from the kernel's start on)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -816,7 +830,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
         // is rounded far below (every sum onto c would round at its size)
         auto products = [&](const i32x8 (&bop)[4], f32x4 (&c)[4]) {
             f32x4 rest[4] = {};
-            if constexpr (LB::kCount > 5) limb_products<BITS, 5, kScaleB>(limb(5), bop, (int)sc[1], rest);
+            limb_products<BITS, 5, kScaleB>(limb(5), bop, (int)sc[1], rest);
             limb_products<BITS, 4, kScaleB>(limb(4), bop, (int)sc[1], rest);
             limb_products<BITS, 3, kScaleB>(limb(3), bop, (int)sc[0], rest);
             limb_products<BITS, 2, kScaleB>(limb(2), bop, (int)sc[0], rest);
@@ -836,7 +850,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
             products(ones, c);
             zs = c[0];
         }
-        WidenNormal<BITS> wide;
+        WidenNormal<BITS, kMiddle> wide;
         wide.init();
         // where the lane writes its weights (rows 4 j + r, tokens 4 n ..) and reads the
         // operand of row n (tokens 32 kc + 8 j ..)
@@ -942,9 +956,12 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
                 for (int t = 0; t < 4; ++t)
                     most = fmaxf(fmaxf(most, fmaxf(x[t][0], x[t][1])), fmaxf(x[t][2], x[t][3]));
                 if (fresh || __any(most > kGrow)) raise_references<D>(s, x, fresh);
-                float vs[4];
+                float vs[4], vz[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) vs[t] = fmaf((float)lo16(pg.vp[t]), vscale, 0.0f);
+                for (int t = 0; t < 4; ++t) {
+                    vs[t] = fmaf((float)lo16(pg.vp[t]), vscale, 0.0f);
+                    vz[t] = fmaf((float)lo16(pg.vp[t]), (float)kMiddle, (float)hi16(pg.vp[t]));
+                }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     uint32_t hi2[2], lo2[2];
@@ -952,7 +969,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         p[t] = fexp2(x[t][r]);
-                        s.z[r] = fmaf(p[t], (float)hi16(pg.vp[t]), s.z[r]);
+                        s.z[r] = fmaf(p[t], vz[t], s.z[r]);
                     }
                     // each part is rounded from the exact product (the hi parts are opaque, so
                     // that the lo parts read them where they are, two to a register)
