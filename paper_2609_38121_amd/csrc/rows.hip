@@ -39,11 +39,11 @@
 // Windows.  q~ and weights in three bf16 parts, 64 slots at a time.
 //
 // What bounds it.  A page of 16 rows is about 415 vector instructions (144 of them the
-// widening of its 8192 value codes), 20 scaled products and 32 fp16 ones, all issued from
-// one port; two workgroups a compute unit keep the vector units 62 to 69% busy.  64
-// sequences on 32768 tokens (d 128, 2-bit, 8 kv heads, G 4): rows_kernel 95 us for 65536
-// page passes, 0.8 us each on a SIMD; 8 sequences of 256 tokens over up to 4000: 175 us;
-// 64 x 16-32K tokens weighted, 128 pages of each: 57 us, 3.5 TB/s of pages.  Tiles of 32
+// widening of its 8192 value codes), 24 scaled products and 32 fp16 ones, all issued from
+// one port; two workgroups a compute unit keep the vector units 58 to 74% busy.  64
+// sequences on 32768 tokens (d 128, 2-bit, 8 kv heads, G 4): rows_kernel 100 us for 65536
+// page passes, 64 a SIMD; 8 sequences of 256 tokens over 1000 to 3000: 183 us; 64
+// sequences weighted, 64 pages of each: 59 us, 3.4 TB/s.  Tiles of 32
 // rows would halve the widening, but at two workgroups a compute unit their registers
 // spill (116 us in the first case), and three workgroups spill with 16 rows.
 #include <algorithm>
