@@ -484,11 +484,18 @@ def _launch_stream(dev, stream):
     return raw(current) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
-def _on_stream(t, stream):
-    """A buffer made here for a call on another stream than the current one
-    stays allocated until that stream has done with it."""
-    if stream is not None:
-        t.record_stream(stream)
+def _on_stream(make, stream):
+    """A buffer made here for a call: on the call's stream, so that it is no block
+    that another stream's launches still use, and kept until the current one, which
+    may read it, has done with it."""
+    if stream is None:
+        return make()
+    torch = _torch()
+    now = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = make()
+    if now != stream:
+        t.record_stream(now)
     return t
 
 
@@ -533,13 +540,13 @@ def wushkv_select_pages(cache: WushKVCache, bounds: WushKVBounds, q, t_k_inv, to
         need = wushkv_select_workspace_bytes(cache, n_q, max_seq_len, top_k)
         if need == 0:
             raise WushKVError(_lib.EINVAL, "wushkv_select_workspace_bytes")
-        workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+        workspace = _on_stream(lambda: torch.empty(need, dtype=torch.uint8, device=q.device), stream)
         space = workspace.data_ptr(), need
     shape = (b, hk, top_k + 1)
     if sel is None:
-        sel = _on_stream(torch.empty(shape, dtype=torch.int32, device=q.device), stream)
+        sel = _on_stream(lambda: torch.empty(shape, dtype=torch.int32, device=q.device), stream)
     if n_sel is None:
-        n_sel = _on_stream(torch.empty(b, hk, dtype=torch.int32, device=q.device), stream)
+        n_sel = _on_stream(lambda: torch.empty(b, hk, dtype=torch.int32, device=q.device), stream)
     st = _lib.lib().wushkv_select_pages(
         ctypes.byref(cache._desc), box, q_at, n_q, max_seq_len, t_at, top_k, _check(dev, sel, "sel", torch.int32, shape),
         _check(dev, n_sel, "n_sel", torch.int32, (b, hk)), scores_at, space[0], space[1], handle)
@@ -571,11 +578,11 @@ def wushkv_sparse_attention(cache: WushKVCache, q, t_k_inv, sel, n_sel, sm_scale
         space = _check_space(dev, workspace)
     handle = _launch_stream(dev, stream)
     if out is None:
-        out = _on_stream(torch.empty(b, n_q, d, dtype=torch.float32, device=q.device), stream)
+        out = _on_stream(lambda: torch.empty(b, n_q, d, dtype=torch.float32, device=q.device), stream)
     if workspace is None:
         # (sizes without a plan: the call says what is wrong)
         need = max(16, wushkv_sparse_workspace_bytes(cache, n_q, max_sel))
-        workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=q.device), stream)
+        workspace = _on_stream(lambda: torch.empty(need, dtype=torch.uint8, device=q.device), stream)
         space = workspace.data_ptr(), need
     st = _lib.lib().wushkv_sparse_attention(
         ctypes.byref(cache._desc), q_at, n_q, sel_at, n_at, max_sel, t_at, float(sm_scale),
@@ -599,7 +606,7 @@ def wushkv_assign_pages(cache: WushKVCache, pool: WushKVPool, source=None, reach
     reach_at = None if reach is None else _check(dev, reach, "reach", torch.int32, shape)
     handle = _launch_stream(dev, stream)
     if status is None:
-        status = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
+        status = _on_stream(lambda: torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
     st = _lib.lib().wushkv_assign_pages(ctypes.byref(cache._desc), books, source_at, reach_at,
                                         _check(dev, status, "status", torch.int32, shape), handle)
     check(st, "wushkv_assign_pages")
@@ -629,10 +636,10 @@ def wushkv_compact_pages(cache: WushKVCache, pool: WushKVPool, bounds=None, tabl
     if refs_out is None:
         refs_out = pool.refs
     if live_out is None:
-        live_out = _on_stream(torch.empty(1, dtype=torch.int32, device=cache.device), stream)
+        live_out = _on_stream(lambda: torch.empty(1, dtype=torch.int32, device=cache.device), stream)
     if workspace is None:
         need = max(16, wushkv_compact_workspace_bytes(cache))
-        workspace = _on_stream(torch.empty(need, dtype=torch.uint8, device=cache.device), stream)
+        workspace = _on_stream(lambda: torch.empty(need, dtype=torch.uint8, device=cache.device), stream)
         space = workspace.data_ptr(), need
     st = _lib.lib().wushkv_compact_pages(
         ctypes.byref(cache._desc), books, box,
@@ -654,9 +661,9 @@ def wushkv_shared_prefixes(cache: WushKVCache, leader=None, shared=None, min_pag
     min_pages = operator.index(min_pages)
     handle = _launch_stream(dev, stream)
     if leader is None:
-        leader = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
+        leader = _on_stream(lambda: torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
     if shared is None:
-        shared = _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
+        shared = _on_stream(lambda: torch.empty(shape, dtype=torch.int32, device=cache.device), stream)
     st = _lib.lib().wushkv_shared_prefixes(ctypes.byref(cache._desc), min_pages,
                                            _check(dev, leader, "leader", torch.int32, shape),
                                            _check(dev, shared, "shared", torch.int32, shape), handle)
@@ -669,13 +676,13 @@ def _rows_call(name, q, out, workspace, need, stream):
     ones; ``need`` gives the workspace's bytes, 0 where the call has no plan."""
     torch = _torch()
     if out is None:
-        out = _on_stream(torch.empty(q.shape, dtype=torch.float32, device=q.device), stream)
+        out = _on_stream(lambda: torch.empty(q.shape, dtype=torch.float32, device=q.device), stream)
     out_at = _check(q.get_device(), out, "out", torch.float32, q.shape)
     if workspace is not None:
         return out, out_at, _check_space(q.get_device(), workspace)
     # (sizes without a plan: the call says what is wrong)
     n = max(16, need())
-    workspace = _on_stream(torch.empty(n, dtype=torch.uint8, device=q.device), stream)
+    workspace = _on_stream(lambda: torch.empty(n, dtype=torch.uint8, device=q.device), stream)
     return out, out_at, (workspace.data_ptr(), n)
 
 
@@ -792,7 +799,7 @@ def wushkv_evict_pages(cache: WushKVCache, pool: WushKVPool, weights, budget, re
         max_sel = sel.shape[2] if sel.dim() == 3 else 0
     max_sel = cache.max_pages if max_sel is None else operator.index(max_sel)
     handle = _launch_stream(dev, stream)
-    new = lambda *shape: _on_stream(torch.empty(shape, dtype=torch.int32, device=cache.device), stream)  # noqa: E731
+    new = lambda *shape: _on_stream(lambda: torch.empty(shape, dtype=torch.int32, device=cache.device), stream)  # noqa: E731
     if sel is None:
         sel = new(b, hk, max(max_sel, 0))
     if n_sel is None:

@@ -181,6 +181,23 @@ def test_other_streams_and_two_at_once(gpu):
     assert torch.equal(out, here[0].out[2]) and torch.equal(cross, here[0].out[1])
 
 
+def test_buffers_made_for_another_stream(gpu):
+    """They are none that the current stream's launches may still use: a block given
+    back here goes out again on this stream alone."""
+    x, side = Calls(gpu, 7), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    held = [torch.zeros(n, dtype=torch.int32, device=gpu) for n in (6, 6, 12 * 8, 6 * 8 * 128, 6 * 8 * 128)]
+    held += [torch.zeros_like(x.space) for _ in range(3)]
+    before = {t.data_ptr() for t in held}
+    del held
+    made = [*wk.wushkv_shared_prefixes(x.c, stream=side)]
+    made += [wk.wushkv_weighted_attention(x.c, x.q, x.t, x.weights, stream=side)]
+    made += [*wk.wushkv_evict_pages(x.c, x.pool, x.weights, dev_i32([9] * 6, gpu), max_sel=12, stream=side)]
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert not {t.data_ptr() for t in made} & before
+
+
 def test_nothing_behind_the_outputs(gpu):
     """Outputs and weights inside larger buffers: what lies round them stays."""
     x = Calls(gpu, 6)
