@@ -650,7 +650,7 @@ size_t wushkv_prefix_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads);
  *   max_tok  (host) >= 1; n_seqs max_tok at most 131072.
  *   source   int32 [n_seqs] device: the stored sequence that query sequence i
  *            attends to (several may name the same: its pages are then read once
- *            for 32 rows of them), or NULL for i (n_seqs at most the batch).
+ *            for 16 rows of them), or NULL for i (n_seqs at most the batch).
  *   out      fp32 of q's shape.  Rows behind n_tok, of a source outside the batch
  *            and of an empty one are zero.
  *   t_k_inv, sm_scale  as wushkv_decode_attention takes them.
