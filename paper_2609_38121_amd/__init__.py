@@ -671,19 +671,21 @@ def wushkv_shared_prefixes(cache: WushKVCache, leader=None, shared=None, min_pag
     return leader, shared
 
 
-def _rows_call(name, q, out, workspace, need, stream):
-    """(out, its address, the workspace's address and bytes): those given, or new
-    ones; ``need`` gives the workspace's bytes, 0 where the call has no plan."""
+def _rows_call(q, out, workspace, need, stream):
+    """(out, its address, the workspace, its address and bytes): those given, or new
+    ones; ``need`` gives the workspace's bytes, 0 where the call has no plan.  The
+    caller keeps both until the library has been called: the block of a tensor that is
+    gone may go to another thread's call before this one's launches."""
     torch = _torch()
     if out is None:
         out = _on_stream(lambda: torch.empty(q.shape, dtype=torch.float32, device=q.device), stream)
     out_at = _check(q.get_device(), out, "out", torch.float32, q.shape)
     if workspace is not None:
-        return out, out_at, _check_space(q.get_device(), workspace)
+        return out, out_at, workspace, _check_space(q.get_device(), workspace)
     # (sizes without a plan: the call says what is wrong)
     n = max(16, need())
     workspace = _on_stream(lambda: torch.empty(n, dtype=torch.uint8, device=q.device), stream)
-    return out, out_at, (workspace.data_ptr(), n)
+    return out, out_at, workspace, (workspace.data_ptr(), n)
 
 
 def wushkv_prefix_workspace_bytes(cache: WushKVCache, n_q_heads: int) -> int:
@@ -707,7 +709,7 @@ def wushkv_prefix_attention(cache: WushKVCache, q, t_k_inv, leader, shared, sm_s
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
     handle = _launch_stream(dev, stream)
-    out, out_at, space = _rows_call("prefix", q, out, workspace, lambda: wushkv_prefix_workspace_bytes(cache, n_q), stream)
+    out, out_at, workspace, space = _rows_call(q, out, workspace, lambda: wushkv_prefix_workspace_bytes(cache, n_q), stream)
     st = _lib.lib().wushkv_prefix_attention(ctypes.byref(cache._desc), q_at, n_q, leader_at, shared_at, t_at,
                                             float(sm_scale), out_at, space[0], space[1], handle)
     check(st, "wushkv_prefix_attention")
@@ -737,8 +739,8 @@ def wushkv_cross_attention(cache: WushKVCache, q, t_k_inv, n_tok=None, source=No
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
     handle = _launch_stream(dev, stream)
-    out, out_at, space = _rows_call("cross", q, out, workspace,
-                                    lambda: wushkv_cross_workspace_bytes(cache, n_seqs, max_tok, n_q), stream)
+    out, out_at, workspace, space = _rows_call(
+        q, out, workspace, lambda: wushkv_cross_workspace_bytes(cache, n_seqs, max_tok, n_q), stream)
     st = _lib.lib().wushkv_cross_attention(ctypes.byref(cache._desc), q_at, n_seqs, n_at, max_tok, source_at, n_q, t_at,
                                            float(sm_scale), out_at, space[0], space[1], handle)
     check(st, "wushkv_cross_attention")
@@ -771,8 +773,8 @@ def wushkv_weighted_attention(cache: WushKVCache, q, t_k_inv, weights, sel=None,
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
     handle = _launch_stream(dev, stream)
-    out, out_at, space = _rows_call("weighted", q, out, workspace,
-                                    lambda: wushkv_weighted_workspace_bytes(cache, n_q, max_sel), stream)
+    out, out_at, workspace, space = _rows_call(
+        q, out, workspace, lambda: wushkv_weighted_workspace_bytes(cache, n_q, max_sel), stream)
     st = _lib.lib().wushkv_weighted_attention(ctypes.byref(cache._desc), q_at, n_q, sel_at, n_at, max_sel, t_at,
                                               float(sm_scale), w_at, out_at, space[0], space[1], handle)
     check(st, "wushkv_weighted_attention")
