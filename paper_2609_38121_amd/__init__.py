@@ -327,9 +327,11 @@ def wushkv_decode_attention(cache: WushKVCache, q, t_k_inv, sm_scale=None, max_s
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(cache.head_dim)
     if out is None:
-        out = torch.empty(cache.batch, n_q, cache.head_dim, dtype=torch.float32, device=q.device)
+        out = _on_stream(lambda: torch.empty(cache.batch, n_q, cache.head_dim, dtype=torch.float32, device=q.device),
+                         stream)
     if workspace is None:
-        workspace = torch.empty(_decode_need(cache, n_q, max_seq_len), dtype=torch.uint8, device=q.device)
+        need = _decode_need(cache, n_q, max_seq_len)
+        workspace = _on_stream(lambda: torch.empty(need, dtype=torch.uint8, device=q.device), stream)
     st = _lib.lib().wushkv_decode_attention(
         ctypes.byref(cache.desc), _ptr(q), n_q, operator.index(max_seq_len), _ptr(t_k_inv),
         float(sm_scale), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -377,9 +379,11 @@ def wushkv_decode_step(cache: WushKVCache, k_new, v_new, n_new, t_k, q, t_k_inv,
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(cache.head_dim)
     if out is None:
-        out = torch.empty(cache.batch, n_q, cache.head_dim, dtype=torch.float32, device=q.device)
+        out = _on_stream(lambda: torch.empty(cache.batch, n_q, cache.head_dim, dtype=torch.float32, device=q.device),
+                         stream)
     if workspace is None:
-        workspace = torch.empty(_decode_need(cache, n_q, max_seq_len), dtype=torch.uint8, device=q.device)
+        need = _decode_need(cache, n_q, max_seq_len)
+        workspace = _on_stream(lambda: torch.empty(need, dtype=torch.uint8, device=q.device), stream)
     st = _lib.lib().wushkv_decode_step(
         ctypes.byref(cache.desc), _ptr(k_new), _ptr(v_new), _ptr(n_new), _ptr(t_k), _ptr(q), n_q,
         operator.index(max_seq_len), _ptr(t_k_inv), float(sm_scale), _ptr(out), _ptr(workspace),
@@ -409,11 +413,11 @@ def wushkv_chunk_attention(cache: WushKVCache, q, t_k_inv, n_tok=None, sm_scale=
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(cache.head_dim)
     if out is None:
-        out = torch.empty(cache.batch, max_tok, n_q, cache.head_dim, dtype=torch.float32,
-                          device=q.device)
+        out = _on_stream(lambda: torch.empty(cache.batch, max_tok, n_q, cache.head_dim, dtype=torch.float32,
+                                             device=q.device), stream)
     if workspace is None:
-        workspace = torch.empty(_chunk_need(cache, n_q, max_tok, max_seq_len), dtype=torch.uint8,
-                                device=q.device)
+        need = _chunk_need(cache, n_q, max_tok, max_seq_len)
+        workspace = _on_stream(lambda: torch.empty(need, dtype=torch.uint8, device=q.device), stream)
     st = _lib.lib().wushkv_chunk_attention(
         ctypes.byref(cache.desc), _ptr(q), _ptr(n_tok), int(max_tok), n_q, operator.index(max_seq_len),
         _ptr(t_k_inv), float(sm_scale), _ptr(out), _ptr(workspace),
@@ -431,9 +435,9 @@ def wushkv_dequant(cache: WushKVCache, b: int, start: int, count: int, k_out=Non
     torch = _torch()
     shape = (cache.n_kv_heads, count, cache.head_dim)
     if k_out is None:
-        k_out = torch.empty(shape, dtype=torch.float32, device=cache.device)
+        k_out = _on_stream(lambda: torch.empty(shape, dtype=torch.float32, device=cache.device), stream)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=torch.float32, device=cache.device)
+        v_out = _on_stream(lambda: torch.empty(shape, dtype=torch.float32, device=cache.device), stream)
     st = _lib.lib().wushkv_dequant(ctypes.byref(cache.desc), int(b), int(start), int(count),
                                    _ptr(k_out), _ptr(v_out), _stream_handle(stream))
     check(st, "wushkv_dequant")
@@ -491,7 +495,7 @@ def _on_stream(make, stream):
     if stream is None:
         return make()
     torch = _torch()
-    now = torch.cuda.current_stream()
+    now = torch.cuda.current_stream(stream.device)
     with torch.cuda.stream(stream):
         t = make()
     if now != stream:
@@ -838,11 +842,11 @@ def wushkv_wush_transform(m, h, gamma: float = 1e-2, t_out=None, t_inv_out=None,
         if t.dtype != torch.float32 or not t.is_contiguous():
             raise ValueError("m and h must be contiguous fp32")
     if t_out is None:
-        t_out = torch.empty_like(m)
+        t_out = _on_stream(lambda: torch.empty_like(m), stream)
     if want_inverse and t_inv_out is None:
-        t_inv_out = torch.empty_like(m)
+        t_inv_out = _on_stream(lambda: torch.empty_like(m), stream)
     if sweeps_out is None:
-        sweeps_out = torch.empty(count, dtype=torch.int32, device=m.device)
+        sweeps_out = _on_stream(lambda: torch.empty(count, dtype=torch.int32, device=m.device), stream)
     st = _lib.lib().wushkv_wush_transform(_ptr(m), _ptr(h), count, d, float(gamma), _ptr(t_out),
                                           _ptr(t_inv_out) if want_inverse else None,
                                           _ptr(sweeps_out), _stream_handle(stream))
@@ -856,7 +860,7 @@ def wushkv_read_probe(buf, mode: int, sink=None, stream=None):
     torch = _torch()
     nbytes = buf.numel() * buf.element_size()
     if sink is None:
-        sink = torch.empty(max(1, nbytes // 65536), dtype=torch.int32, device=buf.device)
+        sink = _on_stream(lambda: torch.empty(max(1, nbytes // 65536), dtype=torch.int32, device=buf.device), stream)
     check(_lib.lib().wushkv_read_probe(_ptr(buf), nbytes, int(mode), _ptr(sink),
                                        _stream_handle(stream)), "wushkv_read_probe")
     return sink
