@@ -288,24 +288,23 @@ __device__ __forceinline__ f32x4 mfma_scaled(const i32x8 &a, const i32x8 &b, int
 // (1024 + c 2^F) 2^(4-F) - 1024 2^(4-F) = 16 c, exactly, from whatever field the
 // page has it in; only fields past the fraction are shifted first.  The
 // constants stay in registers (an instruction takes one that is not).  With a middle
-// they are 16 (c - MIDDLE), as exactly.
-template <int BITS, int MIDDLE = 0>
+// (a whole number below 16, so that each is an fp16 number) they are 16 (c - middle),
+// as exactly.
+template <int BITS>
 struct WidenNormal {
     uint32_t one;       // 1024, twice
-    f16x2 add[5];       // -1024 2^(4-F) - 16 MIDDLE, F = 0, 2, 4, 6, 8
+    f16x2 add[5];       // -1024 2^(4-F) - 16 middle, F = 0, 2, 4, 6, 8
     // -x in fp16, twice
-    static constexpr uint32_t minus(int x)
+    static __device__ __forceinline__ uint32_t minus(float x)
     {
-        int e = 0;
-        while ((2 << e) <= x) ++e;
-        const uint32_t bits = 0x8000u | (uint32_t)(e + 15) << 10 | (uint32_t)(((x << 10) >> e) - 1024);
-        return bits << 16 | bits;
+        const _Float16 y = (_Float16)-x;
+        return __builtin_bit_cast(uint32_t, f16x2{y, y});
     }
-    static_assert(MIDDLE < 64, "one binade each");
-    __device__ __forceinline__ void init()
+    __device__ __forceinline__ void init(float middle = 0.0f)
     {
-        uint32_t v[6] = {0x64006400u, minus(16384 + 16 * MIDDLE), minus(4096 + 16 * MIDDLE), minus(1024 + 16 * MIDDLE),
-                         minus(256 + 16 * MIDDLE), minus(64 + 16 * MIDDLE)};
+        const float m = 16.0f * middle;
+        uint32_t v[6] = {0x64006400u,    minus(16384.0f + m), minus(4096.0f + m),
+                         minus(1024.0f + m), minus(256.0f + m), minus(64.0f + m)};
 #pragma unroll
         for (int i = 0; i < 6; ++i) asm volatile("" : "+v"(v[i]));
         one = v[0];

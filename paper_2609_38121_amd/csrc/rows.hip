@@ -761,8 +761,10 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
     using Lds = RowsLds<D, BITS>;
     constexpr int kNT = L::kNTiles, kC = L::kChunks, kScaleB = BITS == 2 ? 128 : 136;
     constexpr int kPlane = 16 * kPitch;
-    // values as s (c - kMiddle) + (z + kMiddle s): the sums of both are then of the output's size
-    constexpr int kMiddle = BITS == 2 ? 2 : 8;
+    // values as s (c - middle) + (z + middle s): the sums of both are then of the output's size.
+    // (The middle goes by the codes' own bits: three-bit ones, which lie in the four-bit
+    // format, centred on 8 add up to more than raw ones.)
+    const float middle = BITS == 2 ? 2.0f : a.mid + 0.5f;
     // (the lane is opaque where a part begins, so that the addresses that follow from
     // it are formed there, and do not hold registers from the kernel's start on)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -850,8 +852,8 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
             products(ones, c);
             zs = c[0];
         }
-        WidenNormal<BITS, kMiddle> wide;
-        wide.init();
+        WidenNormal<BITS> wide;
+        wide.init(middle);
         // where the lane writes its weights (rows 4 j + r, tokens 4 n ..) and reads the
         // operand of row n (tokens 32 kc + 8 j ..)
         const uint32_t pw = pbuf + 4 * j * kPitch + 8 * n, pr = pbuf + n * kPitch + 16 * j;
@@ -960,7 +962,7 @@ __device__ __forceinline__ void take_tile(const RowsArgs &a, const RowTile &tile
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     vs[t] = fmaf((float)lo16(pg.vp[t]), vscale, 0.0f);
-                    vz[t] = fmaf((float)lo16(pg.vp[t]), (float)kMiddle, (float)hi16(pg.vp[t]));
+                    vz[t] = fmaf((float)lo16(pg.vp[t]), middle, (float)hi16(pg.vp[t]));
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
