@@ -705,11 +705,11 @@ size_t wushkv_weighted_workspace_bytes(const wushkv_cache *c, int32_t n_q_heads,
  *   table_out  int32 [batch][max_pages_per_seq], refs_out int32 [n_pages]: the new
  *            page table and references; either may be the cache's, or the pool's,
  *            own array (in place), and otherwise overlaps none of the call's.
- *   sel, n_sel  nullable, both or neither: int32 [batch][n_kv_heads][max_sel] and
- *            [batch][n_kv_heads]: the lists that the attentions take, of the pages
- *            that are left, the one being filled among them, ascending and -1
- *            behind, the same for every kv head; the newest max_sel where there
- *            are more.
+ *   sel, n_sel  nullable, both or neither (where max_sel is 0, sel alone too): int32
+ *            [batch][n_kv_heads][max_sel] and [batch][n_kv_heads]: the lists that the
+ *            attentions take, of the pages that are left, the one being filled among
+ *            them, ascending and -1 behind, the same for every kv head; the newest
+ *            max_sel where there are more.
  *   max_sel  (host) >= 0, the row length of sel.
  *   evicted  int32 [batch]: pages that left.
  *

@@ -821,8 +821,8 @@ def wushkv_evict_pages(cache: WushKVCache, pool: WushKVPool, weights, budget, re
         ctypes.byref(cache._desc), books, w_at, budget_at, operator.index(recent),
         _check(dev, table_out, "table_out", torch.int32, (b, cache.max_pages)),
         _check(dev, refs_out, "refs_out", torch.int32, (cache.n_pages,)),
-        # (a list of no entries has no address)
-        sel_at if max_sel > 0 else None, _check(dev, n_sel, "n_sel", torch.int32, (b, hk)) if max_sel > 0 else None, max_sel,
+        # (lists of no entries have no address, their counts have)
+        sel_at if max_sel > 0 else None, _check(dev, n_sel, "n_sel", torch.int32, (b, hk)), max_sel,
         _check(dev, evicted, "evicted", torch.int32, (b,)), handle)
     check(st, "wushkv_evict_pages")
     return sel, n_sel, evicted

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(EvictArgs a)
     // (pages left, so that a list that is too short begins later)
     int32_t left = all_live - over;
     if (every > full && lives(row[full])) left += 1;
-    const int32_t skip = max(left - a.max_sel, 0);
+    const int32_t skip = max(left - a.max_sel, 0);  // (all of them where the list has no entries)
     for (int32_t i0 = 0; i0 < mp; i0 += kEvictThreads) {
         const int32_t i = i0 + tid;
         const int32_t phys = i < mp ? row[i] : -1;
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(EvictArgs a)
         }
         if (i < mp && (gone || a.table_out != a.r.page_table)) a.table_out[(int64_t)b * mp + i] = gone ? -1 : phys;
         if (gone && atomicSub(a.refs_out + phys, 1) <= 1) atomicMin(a.low, phys);
-        if (a.sel != nullptr && i0 < every) {
+        if (a.n_sel != nullptr && i0 < every) {
             const bool stays = here && !gone;
             int32_t total;
             const int32_t at = kept_before + evict_scan(stays, sums, total) - skip;
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(EvictArgs a)
         }
     }
     const int32_t listed = min(left, a.max_sel);
-    if (a.sel != nullptr) {
+    if (a.n_sel != nullptr) {
         const int32_t behind = a.max_sel - listed;
         for (int64_t x = tid; x < (int64_t)behind * hk; x += kEvictThreads)
             a.sel[((int64_t)b * hk + x / behind) * a.max_sel + listed + x % behind] = -1;
@@ -270,7 +270,7 @@ extern "C" int wushkv_evict_pages(const wushkv_cache *c, const wushkv_pool *pool
     const int st = wushkv_validate_cache(c);
     if (st != WUSHKV_OK) return st;
     if (!pool || !pool->refs || !pool->held || !pool->low || !weights || !budget || !table_out || !refs_out || !evicted ||
-        recent < 0 || max_sel < 0 || (sel == nullptr) != (n_sel == nullptr))
+        recent < 0 || max_sel < 0 || (sel != nullptr && !n_sel) || (!sel && n_sel && max_sel > 0))
         return WUSHKV_EINVAL;
     if (((uintptr_t)pool->refs | (uintptr_t)pool->held | (uintptr_t)pool->low | (uintptr_t)weights | (uintptr_t)budget |
          (uintptr_t)table_out | (uintptr_t)refs_out | (uintptr_t)sel | (uintptr_t)n_sel | (uintptr_t)evicted) & 15u)
