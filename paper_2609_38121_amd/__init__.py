@@ -234,12 +234,17 @@ class WushKVBounds(_Described):
 class WushKVPool(_Described):
     """The bookkeeping of a cache's pages (wushkv_assign_pages): ``refs`` int32
     [n_pages], ``held`` int32 [batch] and ``low`` int32 [1].  Starts from the
-    cache's page table: every entry of it is one reference."""
+    cache's page table: every entry of it is one reference, and a sequence holds
+    what lies up to its last page and its last quantised position (evicted pages
+    leave holes, which are given no page again)."""
 
     def __init__(self, cache: WushKVCache):
         torch = _torch()
         there = (cache.page_table >= 0) & (cache.page_table < cache.n_pages)
-        self.held = there.sum(1, dtype=torch.int32)
+        number = torch.arange(1, cache.max_pages + 1, dtype=torch.int32, device=cache.device)
+        positions = torch.minimum(cache.quant_end, cache.seq_len) - cache.s_sink
+        stored = torch.div(positions + PAGE_TOKENS - 1, PAGE_TOKENS, rounding_mode="floor").clamp(0, cache.max_pages)
+        self.held = torch.maximum((there * number).amax(1), stored.to(torch.int32))
         pages = cache.page_table[there].long()
         self.refs = torch.bincount(pages, minlength=cache.n_pages).to(torch.int32)
         self.low = torch.zeros(1, dtype=torch.int32, device=cache.device)
