@@ -248,8 +248,9 @@ int wushkv_validate_cache(const wushkv_cache *c);
 
 static PageRows rows_of(const wushkv_cache *c)
 {
+    // (a pool of no pages needs no table; one that is there is copied all the same)
     return PageRows{c->page_table, c->seq_len, c->quant_end, c->batch, c->n_kv_heads, c->s_sink,
-                    c->n_pages > 0 ? c->max_pages_per_seq : 0, c->n_pages};
+                    c->page_table != nullptr ? c->max_pages_per_seq : 0, c->n_pages};
 }
 
 extern "C" int wushkv_shared_prefixes(const wushkv_cache *c, int32_t min_pages, int32_t *leader, int32_t *shared,

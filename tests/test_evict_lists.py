@@ -62,3 +62,27 @@ def test_counts_are_zeros(gpu):
             # (in place first: after it there is nothing more to evict)
             want = [h.complete(b) - 4 if table_out is None and h.complete(b) > 4 else 0 for b in range(3)]
             assert gone.tolist() == want
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[700, 500, 30]])
+def test_a_pool_of_no_pages(gpu, lens):
+    """Nothing leaves, and the new table is the old one."""
+    h = Host(np.random.default_rng(2), lens, 2, 64, 2)
+    c = wk.WushKVCache(3, 2, 64, 2, h.s_sink, h.s_keep, h.s_flush, 0.96, 0.92, max_seq_len=800, win_slots=h.win_slots,
+                       page_order="none", n_pages=0, device=gpu)
+    c.seq_len.copy_(torch.from_numpy(h.seq_len))
+    c.quant_end.copy_(torch.from_numpy(h.quant_end))
+    pool = wk.WushKVPool(c)
+    c.page_table[1, 2] = 3
+    pool.held.fill_(5)
+    at = torch.empty(4, dtype=torch.int32, device=gpu)  # (arrays of no elements have no address)
+    desc = _lib.PoolDesc(at.data_ptr(), pool.held.data_ptr(), pool.low.data_ptr())
+    weights, budget, table = torch.ones(3, 2, c.max_pages, device=gpu), torch.zeros(3, dtype=torch.int32, device=gpu), \
+        torch.full_like(c.page_table, 55)
+    sel, n_sel, gone = ints(3, 2, 4, device=gpu), ints(3, 2, device=gpu), ints(3, device=gpu)
+    assert _lib.lib().wushkv_evict_pages(
+        ctypes.byref(c.desc), ctypes.byref(desc), weights.data_ptr(), budget.data_ptr(), 0, table.data_ptr(), at.data_ptr(),
+        sel.data_ptr(), n_sel.data_ptr(), 4, gone.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(table, c.page_table)
+    assert (sel == -1).all() and (n_sel == 0).all() and (gone == 0).all()
