@@ -1306,6 +1306,7 @@ template <int D>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a)
 {
     __shared__ float sM[8], sL[8];
+    __shared__ int32_t sPage[256], sStep[4];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int32_t G = 1 << a.g_log2;
     const RowTile *tiles = plan_part<const RowTile>(a, h, a.tile_at);
@@ -1339,13 +1340,41 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a)
     // the pages' weights: of a page, its rows' sums brought to their rows' references
     __syncthreads();
     const int32_t end = quantised_end(a, b);
-    for (int32_t u = tid; u < own.n_pages; u += 256) {
-        int32_t lp;
-        if (page_entry(a, b, h, u, end, lp) < 0) continue;
-        const f32x2 *st = reinterpret_cast<const f32x2 *>(a.stat) + (((int64_t)h * a.batch + b) * a.max_sel + u) * G;
+    float *weights = a.weights + ((int64_t)b * a.n_kv + h) * a.max_pages;
+    for (int32_t base = 0; base < own.n_pages; base += 256) {
+        const int32_t u = base + tid;
+        int32_t lp = -1;
+        const bool here = u < own.n_pages && page_entry(a, b, h, u, end, lp) >= 0;
         float w = 0.0f;
-        for (int g = 0; g < G; ++g) w += st[g][0] * fexp2(st[g][1] - sM[g]) / sL[g];
-        atomicAdd(a.weights + ((int64_t)b * a.n_kv + h) * a.max_pages + lp, w);
+        if (here) {
+            const f32x2 *st = reinterpret_cast<const f32x2 *>(a.stat) + (((int64_t)h * a.batch + b) * a.max_sel + u) * G;
+            for (int g = 0; g < G; ++g) w += st[g][0] * fexp2(st[g][1] - sM[g]) / sL[g];
+        }
+        // A list may name a page several times; each adds what it received, in the list's
+        // order, so that the sum is the same in every run: of the round's entries with one
+        // page the n-th adds in step n.  (Ascending lists, as the selection and the eviction
+        // write them, have one step.)
+        int mine = 0, steps = 1;
+        if (a.sel != nullptr) {
+            sPage[tid] = here ? lp : INT32_MAX;
+            __syncthreads();
+            const uint64_t falls = __ballot(here && tid > 0 && sPage[tid - 1] >= lp);
+            if (lane == 0) sStep[wave] = falls != 0;
+            __syncthreads();
+            if ((sStep[0] | sStep[1] | sStep[2] | sStep[3]) != 0) {
+                const int n = min(own.n_pages - base, 256);
+                for (int i = 0; i < n; ++i) mine += i < tid && sPage[i] == lp;
+                __syncthreads();  // (read, those of the test too)
+                const int most = (int)wave_max(here ? (float)mine : 0.0f);
+                if (lane == 0) sStep[wave] = most;
+                __syncthreads();
+                steps = 1 + max(max(sStep[0], sStep[1]), max(sStep[2], sStep[3]));
+            }
+        }
+        for (int k = 0; k < steps; ++k) {
+            if (here && mine == k) weights[lp] += w;
+            if (a.sel != nullptr) __syncthreads();  // (and the round's pages are read)
+        }
     }
 }
 
