@@ -13,6 +13,7 @@ from gpu_harness import say
 from pages_ref import Host
 from test_gpu_pages import bf16, dev_i32
 from test_gpu_rows import f32, fork, queries
+from workloads import synth
 
 pytestmark = pytest.mark.gpu
 
@@ -26,8 +27,8 @@ def check(what, got, want, s):
     assert most <= 1.0 and rms <= 1.0
 
 
-def all_of_them(gpu, h, q, t, sel, n, leader, shared, x, source):
-    c, _ = h.cache(gpu)
+def all_of_them(gpu, h, q, t, sel, n, leader, shared, x, source, c=None):
+    c = h.cache(gpu)[0] if c is None else c
     qd, td = bf16(q, gpu), f32(t, gpu)
     for name, more in (("every page", ()), ("listed", (sel, n))):
         w = torch.zeros(h.b, h.hk, h.max_pages, device=gpu)
@@ -67,3 +68,31 @@ def test_random(gpu, lens, d, bits, G, hk):
     q, t = queries(rng, 5, hk * G, d), pages_ref.transform(rng, hk, d)
     all_of_them(gpu, h, q, t, *sparse_exact.lists(rng, h, 9), np.array([0, 1, 0, 3, 2]), shared,
                 queries(rng, 7, 5, hk * G, d), np.array([0, 4, 2, 0, 1, 3, 2]))
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4])
+@pytest.mark.parametrize("codec", ["quest", "pclip"])
+def test_appended_tokens(gpu, codec, bits):
+    """A cache of either codec as the append fills it."""
+    say("%s, %d-bit" % (codec, bits))
+    rng = np.random.default_rng([bits, len(codec)])
+    lens, hk, G, d = [600, 257, 333, 3, 90], 2, 4, 128
+    c = wk.WushKVCache(5, hk, d, bits, 4, 64, 8, 0.96, 0.92, max_seq_len=700, codec=codec, device=gpu)
+    t = pages_ref.transform(rng, hk, d)
+    k, v = (bf16(synth.to_bf16_bits(rng.standard_normal((5, 600, hk, d))), gpu) for _ in range(2))
+    tk = bf16(synth.to_bf16_bits(np.stack([np.linalg.inv(x.astype(np.float64)).T for x in t])), gpu)
+    wk.wushkv_append(c, k, v, dev_i32(lens, gpu), tk)
+    h = object.__new__(Host)
+    h.b, h.hk, h.d, h.bits, h.s_sink, h.s_keep, h.s_flush, h.win_slots = 5, hk, d, bits, 4, 64, 8, c.win_slots
+    h.max_pages, h.n_pages = c.max_pages, c.n_pages
+    h.table, h.seq_len, h.quant_end = (x.cpu().numpy() for x in (c.page_table, c.seq_len, c.quant_end))
+    h.pages = c.pages.cpu().numpy().reshape(c.n_pages, hk, -1)
+    h.win_k, h.win_v = (x.view(torch.int16).cpu().numpy().view(np.uint16) for x in (c.win_k, c.win_v))
+    assert h.complete(0) >= 7
+    shared = np.array([0, 3, 4, 0, 0])
+    fork(h, 1, 0, shared[1])
+    fork(h, 2, 0, shared[2])
+    c.page_table.copy_(torch.from_numpy(h.table))
+    sel, n = sparse_exact.lists(rng, h, 6)
+    all_of_them(gpu, h, queries(rng, 5, hk * G, d), t, sel, n, np.array([0, 0, 0, 3, 4]), shared, queries(rng, 3, 4, hk * G, d),
+                np.array([2, 0, 4]), c)
