@@ -1306,7 +1306,9 @@ template <int D>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a)
 {
     __shared__ float sM[8], sL[8];
+    constexpr int kPlaces = 4096;
     __shared__ int32_t sPage[256], sStep[4];
+    __shared__ uint8_t sLast[kPlaces];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int32_t G = 1 << a.g_log2;
     const RowTile *tiles = plan_part<const RowTile>(a, h, a.tile_at);
@@ -1352,19 +1354,22 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a)
         }
         // A list may name a page several times; each adds what it received, in the list's
         // order, so that the sum is the same in every run: of the round's entries with one
-        // page the n-th adds in step n.  (Ascending lists, as the selection and the eviction
-        // write them, have one step.)
+        // page the n-th adds in step n.  Whether there is more than one step at all: every
+        // entry leaves its number in its page's place, and finds it there if no other has
+        // that place (pages 4096 apart have the same one; they only take the longer way).
+        // (64 sequences, 64 entries: 68.9 us a call in any order, 72 with every page twice.)
         int mine = 0, steps = 1;
         if (a.sel != nullptr) {
-            sPage[tid] = here ? lp : INT32_MAX;
+            sPage[tid] = here ? lp : -1;
+            if (here) sLast[lp % kPlaces] = (uint8_t)tid;
             __syncthreads();
-            const uint64_t falls = __ballot(here && tid > 0 && sPage[tid - 1] >= lp);
-            if (lane == 0) sStep[wave] = falls != 0;
+            const uint64_t again = __ballot(here && sLast[lp % kPlaces] != tid);
+            if (lane == 0) sStep[wave] = again != 0;
             __syncthreads();
             if ((sStep[0] | sStep[1] | sStep[2] | sStep[3]) != 0) {
                 const int n = min(own.n_pages - base, 256);
                 for (int i = 0; i < n; ++i) mine += i < tid && sPage[i] == lp;
-                __syncthreads();  // (read, those of the test too)
+                __syncthreads();  // (the tests are read)
                 const int most = (int)wave_max(here ? (float)mine : 0.0f);
                 if (lane == 0) sStep[wave] = most;
                 __syncthreads();
