@@ -28,7 +28,7 @@
  *                            pages in use moved to the front of the pool
  *   wushkv_shared_prefixes, wushkv_prefix_attention
  *                            the pages that sequences share at their start
- *                            attended to once for all of them
+ *                            attended to together, 16 query rows at a time
  *   wushkv_cross_attention   queries of other sequences, of any length, over
  *                            whole stored ones
  *   wushkv_weighted_attention, wushkv_evict_pages
@@ -614,8 +614,11 @@ int wushkv_shared_prefixes(const wushkv_cache *c, int32_t min_pages, int32_t *le
 
 /*
  * wushkv_prefix_attention -- wushkv_decode_attention for sequences that share
- * pages at their start: a page that several have is read and attended to once for
- * all of their query rows.
+ * pages at their start: a page that several have is read once for 16 of their query
+ * rows (and from memory about once).  It is the faster call where most of what the
+ * batch attends to is shared, and the slower one otherwise: with 64 sequences, 8 kv
+ * heads of four query heads and 1000 tokens of their own each it takes 60 us where
+ * the decode takes 74 at 8192 shared tokens (2-bit), and 50 where that takes 45 at 2048.
  *
  *   q, n_q_heads, t_k_inv, sm_scale, out  as wushkv_decode_attention takes them.
  *   leader, shared  int32 [batch] device, as wushkv_shared_prefixes gives them.

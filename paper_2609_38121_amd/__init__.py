@@ -704,8 +704,9 @@ def wushkv_prefix_workspace_bytes(cache: WushKVCache, n_q_heads: int) -> int:
 def wushkv_prefix_attention(cache: WushKVCache, q, t_k_inv, leader, shared, sm_scale=None, out=None, workspace=None,
                             stream=None):
     """wushkv_decode_attention for sequences that share pages at their start,
-    which are attended to once for all of them: leader, shared int32 [batch]
-    (wushkv_shared_prefixes).  q: bf16 [batch][n_q][d]; t_k_inv: fp32
+    which are attended to together, 16 query rows at a time: leader, shared int32
+    [batch] (wushkv_shared_prefixes).  The faster of the two where most of what the
+    batch attends to is shared.  q: bf16 [batch][n_q][d]; t_k_inv: fp32
     [n_kv][d][d].  Returns fp32 [batch][n_q][d]."""
     torch = _torch()
     dev = cache.pages.get_device()

@@ -12,9 +12,9 @@
 // array, a launch before it copies them.
 //
 // Both are a launch and chains of dependent reads: 64 sequences that share 8-32K tokens
-// with 15 others 5.3 us, of 8 forks 4.0; eviction from 64 sequences of 16-32K tokens, 8 kv
+// with 15 others 6.4 us, of 8 forks 3.6; eviction from 64 sequences of 16-32K tokens, 8 kv
 // heads, 14.3 us (1 MB of weights; a workgroup of 1024 a sequence, so that a row's keys stay
-// in LDS and no launch lies between its rounds) and the copy 2.1.
+// in LDS and no launch lies between its rounds) and the copy 1.9.
 #include "common.h"
 #include "merge.h"
 

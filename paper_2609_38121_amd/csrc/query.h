@@ -71,9 +71,10 @@ struct TColumns {
 // l supplies A = q[l % 16][k0 + l / 16] and
 // B = T^{-1}[k0 + l / 16][n0 + l % 16] and holds the result rows
 // 4 (l / 16) .. + 3 of column n0 + l % 16.  The T^{-1} column entries of
-// all steps come loaded in tc.  Same contract as form_qt (q~ scaled,
-// fp32, into R; starts and ends with a barrier); the products are summed in
-// the matrix unit's order, so q~ may differ from form_qt's in the last bits.
+// all steps come loaded in tc.  Same contract as form_qt in decode.hip (q~
+// scaled, fp32, into R; starts and ends with a barrier); the products are
+// summed in the matrix unit's order, so q~ may differ from form_qt's in the
+// last bits.
 template <int D, int G>
 __device__ __forceinline__ void form_qt_mfma(float scale, const TColumns<D> &tc, uint8_t *R, int tid)
 {
@@ -99,8 +100,8 @@ __device__ __forceinline__ void form_qt_mfma(float scale, const TColumns<D> &tc,
     __syncthreads();
 }
 
-// Rewrites q~ in R (form_qt) as the operands of the quantised-key product:
-// one wave per query head writes q~ in fixed point, N = rne(q~ 2^F) with F
+// Rewrites q~ in R (form_qt_mfma, form_qt) as the operands of the
+// quantised-key product: one wave per query head writes q~ in fixed point, N = rne(q~ 2^F) with F
 // the largest exponent that keeps |N| <= kNMax, as balanced digits (N =
 // sum_l d_l base^(kCount - 1 - l)).  Each digit is an integer of its number
 // format and limb l carries the E8M0 scale base^(kCount - 1 - l) 2^-F, so
@@ -235,7 +236,7 @@ __device__ __forceinline__ uint32_t lds_addr(const void *p)
 
 // LDS reads and writes are ordinary loads and stores, so the compiler tracks
 // their completion (and any register copies of their results) itself.  The
-// direct-to-LDS page loads are not visible to it (dma16 below): it would
+// direct-to-LDS page loads (dma16 in decode.hip) are not visible to it: it would
 // otherwise wait for every one of them before any LDS access, since it
 // cannot tell the staging slots apart from the rest of LDS.  Ordering
 // against those loads is explicit: wait_vmcnt_at_most before a slot is read,

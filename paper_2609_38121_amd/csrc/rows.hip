@@ -32,19 +32,20 @@
 // softmax has a reference, a whole number, at its maximum of the time, that moves only
 // when a weight would pass 2^kGrow, so that a page costs one test.  Weights
 // p s go through LDS as fp16 hi + lo parts, each formed from the exact product, to
-// be the rows of the P V products with the value codes as fp16 numbers 16 (c - middle).  The
-// value scales are brought to about one by a power of two that the wave keeps
-// (tiny scales would leave the lo parts no bits); sums of p (z + middle s) and p are fp32.
+// be the rows of the P V products with the value codes as fp16 numbers 16 (c - middle),
+// middle that of the codes' own bits.  The value scales are brought to about one by a power
+// of two that the wave keeps (tiny scales would leave the lo parts no bits); sums of
+// p (z + middle s) and p are fp32.
 //
 // Windows.  q~ and weights in three bf16 parts, 64 slots at a time.
 //
 // What bounds it.  A page of 16 rows is about 415 vector instructions (144 of them the
 // widening of its 8192 value codes), 24 scaled products and 32 fp16 ones, all issued from
-// one port; two workgroups a compute unit keep the vector units 58 to 74% busy.  64
-// sequences on 32768 tokens (d 128, 2-bit, 8 kv heads, G 4): rows_kernel 100 us for 65536
-// page passes, 64 a SIMD; 8 sequences of 256 tokens over 1000 to 3000: 183 us; 64
-// sequences weighted, 64 pages of each: 59 us, 3.4 TB/s.  Tiles of 32
-// rows would halve the widening, but at two workgroups a compute unit their registers
+// one port; two workgroups a compute unit keep the vector units 59 to 74% busy.  64
+// sequences on 32768 tokens (d 128, 2-bit, 8 kv heads, G 4): rows_kernel 103 us for 65536
+// page passes, 64 a SIMD; 8 sequences of 256 tokens over 1000 to 3000: 197 us; 64
+// sequences weighted, 64 pages of each: 60 us, 3.4 TB/s (in traces of eight calls).  Tiles
+// of 32 rows would halve the widening, but at two workgroups a compute unit their registers
 // spill (116 us in the first case), and three workgroups spill with 16 rows.
 #include <algorithm>
 #include <atomic>
