@@ -65,3 +65,35 @@ def test_pages_listed_several_times(gpu, kind, d, bits, G, hk, width):
     assert off <= 1.0 and (diff <= slack).all()
     for out, w in runs[1:]:
         assert np.array_equal(out, runs[0][0]) and np.array_equal(w, runs[0][1])
+
+
+def test_pages_far_apart(gpu):
+    """Pages that differ by multiples of 4096, once and several times, and the last of a
+    long row."""
+    rng = np.random.default_rng(77)
+    h = Host(rng, [64 * 5 + 40, 64 * 5 + 40], 2, 64, 2)
+    n = 9000
+    used = h.used
+    h.max_pages, h.table = n, rng.choice(used, (2, n)).astype(np.int32)
+    h.quant_end = np.array([4 + 64 * n - 9, 4 + 64 * 8200], np.int32)
+    h.seq_len = h.quant_end + 40
+    q, t = queries(rng, 2, 4, 64), pages_ref.transform(rng, 2, 64)
+    sel = np.stack([np.concatenate([rng.permutation([5, 4101, 8197, 5 + 1, 4102, 8198, n - 1, n - 2, 4096, 0, 8192, 8500]),
+                                    rng.integers(0, n, 288)]) for _ in range(4)]).reshape(2, 2, 300).astype(np.int32)
+    sel[1, 0, 200:240] = sel[1, 0, 40]
+    weights = rng.exponential(1.0, (2, 2, n)).astype(np.float32)
+    c, _ = h.cache(gpu)
+    runs = []
+    for _ in range(5):
+        w = f32(weights, gpu)
+        out = wk.wushkv_weighted_attention(c, bf16(q, gpu), f32(t, gpu), w, dev_i32(sel, gpu), dev_i32(np.full((2, 2), 300), gpu))
+        runs.append((out.cpu().numpy(), w.cpu().numpy()))
+    want, s, e, new, slack = rows_exact.weighted(h, q, t, weights, sel, np.full((2, 2), 300))
+    for b in range(2):
+        for i in range(2):
+            more = np.bincount(sel[b, i], minlength=n)
+            slack[b, i] += np.maximum(more - 1.0, 0.0) * rows_exact.U * new[b, i]  # (as above)
+    assert rows_exact.off(runs[0][0], want, s, e) <= 1.0
+    assert (np.abs(runs[0][1].astype(np.float64) - new) <= slack).all()
+    for out, w in runs[1:]:
+        assert np.array_equal(out, runs[0][0]) and np.array_equal(w, runs[0][1])
